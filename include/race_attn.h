@@ -217,6 +217,91 @@ race_status_t race_attn_step(const race_attn_desc_t *desc, const void *q, const 
                              const uint64_t *proj_seeds, float *state, void *o, float *den,
                              void *workspace, size_t workspace_bytes, race_stream_t stream);
 
+/* ---- The gated delta rule: a second linear-time layer with a carried state, for models that hold layers of both kinds.
+ * Per value head, with decay a_t = exp(g_t) and write strength b_t = beta_t, from the state S_0 in R^{dk x dv}:
+ *     S_t = a_t S_{t-1} + k_t b_t (v_t - a_t S_{t-1}^T k_t)^T,     o_t = scale * S_t^T q_t.
+ * Conventions
+ *   - Q, K, dQ, dK are DEVICE (B, Hk, N, dk), V, O, dO, dV DEVICE (B, H, N, dv) arrays, row-major, of the element type desc->dtype;
+ *     g, beta, dg, dbeta are DEVICE float (B, H, N); states are DEVICE float (B, H, dk, dv).  Value head h reads the queries and keys of
+ *     head h / (H / Hk); their gradients are summed over the value heads that share them.
+ *   - g is the logarithm of the decay, usually <= 0; -infinity (every value below -1e5) empties the state before the token is written.  beta is
+ *     used as given.  Rows of Q and K are used as given: a bounded state wants |k| <= 1 with beta in [0, 2] (race_qk_rotary_fwd makes such rows).
+ *   - A padding token is one with g = 0 and beta = 0: the state passes it unchanged; its rows must be finite.
+ *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64).  The bf16 type multiplies states and
+ *     their cotangents as the sum of two bf16; O, dQ, dK and dV are rounded to bf16 at the end.
+ *   - A non-finite element of Q, K, V or dO reaches what depends on it, and may spread over the 64 tokens of its chunk, for bf16 and
+ *     fp32 alike; it does not reach another head or sequence (Q, K: other than those that share them).
+ *   - Pointers need be aligned to their elements only.  Buffers must not overlap, except that a state may be carried in place: state_out
+ *     may be state_in, dstate_in may be dstate_out.
+ *   - Everything else (workspace, streams, errors, capture into a graph) as above.  Results are the same bits every time. */
+typedef struct {
+    int32_t B, H, Hk; /* batch, value heads, heads of queries and keys (H a multiple of Hk)             */
+    int64_t N;        /* tokens per sequence (>= 0)                                                     */
+    int32_t dk, dv;   /* multiples of 8, 8 .. 128.  (A wider value row: two value heads of half of it, with the same g, beta and shared q, k) */
+    float scale;      /* of the outputs, finite                                                         */
+    int32_t dtype;    /* race_dtype_t                                                                   */
+    int64_t chunk;    /* tokens per scan segment, rounded up to whole chunks; 0 = choose                */
+} race_delta_desc_t;
+
+/* Bytes of device workspace of race_delta_fwd and of race_delta_bwd.  0 for an invalid or unsupported descriptor and for N == 0. */
+size_t race_delta_workspace_bytes(const race_delta_desc_t *desc);
+size_t race_delta_bwd_workspace_bytes(const race_delta_desc_t *desc);
+/* Bytes of one state (B, H, dk, dv are used); 0 for an invalid descriptor. */
+size_t race_delta_state_bytes(const race_delta_desc_t *desc);
+/* Tokens per scan segment the library uses for this descriptor.  Informational.  0 = invalid. */
+int64_t race_delta_segment_tokens(const race_delta_desc_t *desc);
+
+/* Forward pass.  state_in: state before the first token, NULL = zero.  state_out: state behind the last token, NULL = not wanted.
+ * N == 0: state_out is state_in. */
+race_status_t race_delta_fwd(const race_delta_desc_t *desc, const void *Q, const void *K, const void *V, const float *g, const float *beta,
+                             const float *state_in, void *O, float *state_out, void *workspace, size_t workspace_bytes,
+                             race_stream_t stream);
+
+/* Backward pass on the forward pass's inputs (it needs nothing that the forward pass left behind).  dstate_out: cotangent of state_out,
+ * NULL = zero.  dstate_in: cotangent of state_in, NULL = not wanted.  N == 0: dstate_in is dstate_out. */
+race_status_t race_delta_bwd(const race_delta_desc_t *desc, const void *Q, const void *K, const void *V, const float *g, const float *beta,
+                             const float *state_in, const void *dO, const float *dstate_out, void *dQ, void *dK, void *dV, float *dg,
+                             float *dbeta, float *dstate_in, void *workspace, size_t workspace_bytes, race_stream_t stream);
+
+/* One token per sequence: q, k DEVICE (B, Hk, dk), v, o DEVICE (B, H, dv), g, beta DEVICE float (B, H); the state is updated in place and then read.
+ * desc->N and desc->chunk are ignored.  One kernel, no workspace. */
+race_status_t race_delta_step(const race_delta_desc_t *desc, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                              float *state, void *o, race_stream_t stream);
+
+/* ---- Rows of queries and keys for the layers above: norm for each head and position rotation in one pass.
+ * The row x (d elements) of a token and head becomes rotate(x * r * w), r = 1 / sqrt(mean x^2 + eps) (RACE_NORM_RMS), 1 / sqrt(sum x^2 + eps)
+ * (RACE_NORM_L2) or 1; rotate turns pair i = 0 .. rot/2 - 1 of the first rot elements, (x_i, x_{i + rot/2}) or with
+ * neighbours = 1 (x_{2i}, x_{2i+1}), by the angle position * inv_freq[i]: (m cos - n sin, n cos + m sin).
+ *   - The rows as given are read where they lie, e.g. in the output (B, N, heads * d) of a fused projection: element e of the row of (b, n, head) is
+ *     at b * strides[0] + n * strides[1] + head * strides[2] + e.  Q and K are contiguous (B, Hq, N, d) and (B, Hk, N, d), as the layers take them.
+ *   - wq, wk: DEVICE float (d), NULL = ones.  inv_freq: HOST, rot/2 finite doubles, read during the call.  positions: DEVICE int64 (B, N), NULL =
+ *     pos0 + n.  Angles are formed in fp64.
+ *   - Arithmetic is fp32, rounded once to desc->dtype.  A non-finite element spreads over its own row.  Pointers need be aligned to their elements only. */
+typedef enum { RACE_NORM_NONE = 0, RACE_NORM_RMS = 1, RACE_NORM_L2 = 2 } race_norm_t;
+typedef struct {
+    int32_t B, Hq, Hk;     /* batch, heads of queries (>= 1) and keys (>= 0)                                  */
+    int64_t N;             /* tokens per sequence (>= 0)                                                      */
+    int32_t d, rot;        /* row: multiple of 8, 8 .. 256; rotated elements: even, 0 .. d                    */
+    int32_t norm;          /* race_norm_t                                                                     */
+    int32_t neighbours;    /* 0: pairs (i, i + rot/2), 1: pairs (2i, 2i + 1)                                  */
+    float eps;             /* >= 0, finite                                                                    */
+    int32_t dtype;         /* race_dtype_t of rows, Q, K and their cotangents                                 */
+    int64_t pos0;          /* position of token 0 where positions is NULL                                     */
+    int64_t q_strides[3], k_strides[3];    /* batch, token, head of the rows as given, elements, >= 0         */
+    int64_t dq_strides[3], dk_strides[3];  /* the same of their cotangents (backward only): rows must not overlap */
+} race_rotary_desc_t;
+
+/* k, K, wk may be NULL with Hk = 0. */
+race_status_t race_qk_rotary_fwd(const race_rotary_desc_t *desc, const void *q, const void *k, const float *wq, const float *wk,
+                                 const double *inv_freq, const int64_t *positions, void *Q, void *K, race_stream_t stream);
+
+/* Backward pass: dq, dk from dQ, dK and the rows as given.  dwq, dwk (DEVICE float (d)): NULL = not wanted; sums in a fixed
+ * order.  Workspace: race_qk_rotary_workspace_bytes(), needed only with dwq or dwk. */
+size_t race_qk_rotary_workspace_bytes(const race_rotary_desc_t *desc);
+race_status_t race_qk_rotary_bwd(const race_rotary_desc_t *desc, const void *q, const void *k, const float *wq, const float *wk,
+                                 const double *inv_freq, const int64_t *positions, const void *dQ, const void *dK, void *dq, void *dk,
+                                 float *dwq, float *dwk, void *workspace, size_t workspace_bytes, race_stream_t stream);
+
 /* Static, never-null description of a status code. */
 const char *race_status_string(race_status_t status);
 

@@ -25,6 +25,20 @@ class RaceAttnDesc(ctypes.Structure):
                 ("unit_qk", ctypes.c_int32)]
 
 
+class RaceDeltaDesc(ctypes.Structure):
+    """race_delta_desc_t"""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int64), ("dk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("chunk", ctypes.c_int64)]
+
+
+class RaceRotaryDesc(ctypes.Structure):
+    """race_rotary_desc_t"""
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int64), ("d", ctypes.c_int32),
+                ("rot", ctypes.c_int32), ("norm", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("dtype", ctypes.c_int32), ("pos0", ctypes.c_int64), ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3),
+                ("dq_strides", ctypes.c_int64 * 3), ("dk_strides", ctypes.c_int64 * 3)]
+
+
 class RaceAttnError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -86,6 +100,17 @@ def lib() -> ctypes.CDLL:
         L.race_attn_step.restype = ctypes.c_int
         L.race_attn_calibration_mfma.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, fp, vp]
         L.race_attn_calibration_mfma.restype = ctypes.c_int
+        ddp, rdp, sz = ctypes.POINTER(RaceDeltaDesc), ctypes.POINTER(RaceRotaryDesc), ctypes.c_size_t
+        for name in ("race_delta_workspace_bytes", "race_delta_bwd_workspace_bytes", "race_delta_state_bytes"):
+            getattr(L, name).argtypes, getattr(L, name).restype = [ddp], sz
+        L.race_delta_segment_tokens.argtypes, L.race_delta_segment_tokens.restype = [ddp], ctypes.c_int64
+        L.race_delta_fwd.argtypes, L.race_delta_fwd.restype = [ddp] + [vp] * 9 + [sz, vp], ctypes.c_int
+        L.race_delta_bwd.argtypes, L.race_delta_bwd.restype = [ddp] + [vp] * 15 + [sz, vp], ctypes.c_int
+        L.race_delta_step.argtypes, L.race_delta_step.restype = [ddp] + [vp] * 8, ctypes.c_int
+        L.race_qk_rotary_workspace_bytes.argtypes, L.race_qk_rotary_workspace_bytes.restype = [rdp], sz
+        f64p = ctypes.POINTER(ctypes.c_double)
+        L.race_qk_rotary_fwd.argtypes, L.race_qk_rotary_fwd.restype = [rdp] + [vp] * 4 + [f64p] + [vp] * 4, ctypes.c_int
+        L.race_qk_rotary_bwd.argtypes, L.race_qk_rotary_bwd.restype = [rdp] + [vp] * 4 + [f64p] + [vp] * 8 + [sz, vp], ctypes.c_int
         L.race_status_string.argtypes = [ctypes.c_int]
         L.race_status_string.restype = ctypes.c_char_p
         L.race_attn_last_error.argtypes = []
@@ -349,3 +374,115 @@ def race_attn_profile_read(max_entries: int = 32):
     cnt = (ctypes.c_int * max_entries)()
     n = min(lib().race_attn_profile_read(max_entries, names, ms, cnt), max_entries)
     return {names[i].decode(): (float(ms[i]), int(cnt[i])) for i in range(n)}
+
+
+# ---- the gated delta rule
+
+def make_delta_desc(B: int, H: int, Hk: int, N: int, dk: int, dv: int, scale: float, dtype: int, chunk: int = 0) -> RaceDeltaDesc:
+    return RaceDeltaDesc(B, H, Hk, N, dk, dv, float(scale), int(dtype), int(chunk))
+
+
+def race_delta_workspace_bytes(desc: RaceDeltaDesc) -> int:
+    return int(lib().race_delta_workspace_bytes(ctypes.byref(desc)))
+
+
+def race_delta_bwd_workspace_bytes(desc: RaceDeltaDesc) -> int:
+    return int(lib().race_delta_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def race_delta_state_bytes(desc: RaceDeltaDesc) -> int:
+    return int(lib().race_delta_state_bytes(ctypes.byref(desc)))
+
+
+def race_delta_segment_tokens(desc: RaceDeltaDesc) -> int:
+    return int(lib().race_delta_segment_tokens(ctypes.byref(desc)))
+
+
+def _scratch(need, device):
+    return _torch().empty(max(need, 256), dtype=_torch().uint8, device=device)
+
+
+def race_delta_fwd(desc: RaceDeltaDesc, Q, K, V, g, beta, state_in=None, O=None, state_out=None, want_state: bool = False, workspace=None,
+                   stream=None):
+    """Returns O (B, H, N, dv) and the state behind the sequence, (B, H, dk, dv) float32 (None unless state_out or want_state is given)."""
+    if O is None:
+        O = _torch().empty_like(V)
+    if state_out is None and want_state:
+        state_out = _torch().empty((desc.B, desc.H, desc.dk, desc.dv), dtype=_torch().float32, device=V.device)
+    if workspace is None:
+        workspace = _scratch(race_delta_workspace_bytes(desc), V.device)
+    st = (_native_module or _native()).delta_fwd(desc, Q, K, V, g, beta, state_in, O, state_out, workspace, stream)
+    if st != RACE_OK:
+        raise RaceAttnError(st, "race_delta_fwd")
+    return O, state_out
+
+
+def race_delta_bwd(desc: RaceDeltaDesc, Q, K, V, g, beta, dO, state_in=None, dstate_out=None, dQ=None, dK=None, dV=None, dg=None, dbeta=None,
+                   dstate_in=None, want_dstate: bool = False, workspace=None, stream=None):
+    """Returns dQ, dK, dV, dg, dbeta and the cotangent of state_in (None unless dstate_in or want_dstate is given)."""
+    torch = _torch()
+    dQ, dK, dV, dg, dbeta = (torch.empty_like(x) if y is None else y for x, y in ((Q, dQ), (K, dK), (V, dV), (g, dg), (beta, dbeta)))
+    if dstate_in is None and want_dstate:
+        dstate_in = torch.empty((desc.B, desc.H, desc.dk, desc.dv), dtype=torch.float32, device=V.device)
+    if workspace is None:
+        workspace = _scratch(race_delta_bwd_workspace_bytes(desc), V.device)
+    st = (_native_module or _native()).delta_bwd(desc, Q, K, V, g, beta, state_in, dO, dstate_out, dQ, dK, dV, dg, dbeta, dstate_in, workspace, stream)
+    if st != RACE_OK:
+        raise RaceAttnError(st, "race_delta_bwd")
+    return dQ, dK, dV, dg, dbeta, dstate_in
+
+
+def race_delta_step(desc: RaceDeltaDesc, q, k, v, g, beta, state, o=None, stream=None):
+    """One token: q, k (B, Hk, dk), v (B, H, dv), g, beta (B, H); the state is updated in place; returns o (B, H, dv)."""
+    if o is None:
+        o = _torch().empty_like(v)
+    st = (_native_module or _native()).delta_step(desc, q, k, v, g, beta, state, o, stream)
+    if st != RACE_OK:
+        raise RaceAttnError(st, "race_delta_step")
+    return o
+
+
+# ---- rows of queries and keys
+
+_NORMS, _PAIRS = {"none": 0, "rms": 1, "l2": 2}, {"halves": 0, "neighbours": 1}
+
+
+def make_rotary_desc(B: int, N: int, Hq: int, Hk: int, d: int, rot: int, dtype: int, norm: str = "rms", pairs: str = "halves", eps: float = 1e-6,
+                     pos0: int = 0) -> RaceRotaryDesc:
+    """The strides are those of the tensors that a call is given."""
+    if norm not in _NORMS or pairs not in _PAIRS:
+        raise ValueError("norm must be one of %s, pairs one of %s" % (tuple(_NORMS), tuple(_PAIRS)))
+    return RaceRotaryDesc(B=B, Hq=Hq, Hk=Hk, N=N, d=d, rot=rot, norm=_NORMS[norm], neighbours=_PAIRS[pairs], eps=float(eps), dtype=int(dtype), pos0=int(pos0))
+
+
+def race_qk_rotary_workspace_bytes(desc: RaceRotaryDesc) -> int:
+    return int(lib().race_qk_rotary_workspace_bytes(ctypes.byref(desc)))
+
+
+def race_qk_rotary_fwd(desc: RaceRotaryDesc, q, k, wq, wk, inv_freq: Sequence[float], positions=None, Q=None, K=None, stream=None):
+    """q (B, N, Hq, d) and k (B, N, Hk, d), views with any strides but 1 in the last dimension; returns Q (B, Hq, N, d) and K (B, Hk, N, d)."""
+    if Q is None:
+        Q = _torch().empty((desc.B, desc.Hq, desc.N, desc.d), dtype=q.dtype, device=q.device)
+    if K is None and desc.Hk > 0:
+        K = _torch().empty((desc.B, desc.Hk, desc.N, desc.d), dtype=k.dtype, device=k.device)
+    st = (_native_module or _native()).rotary_fwd(desc, q, k, wq, wk, inv_freq, positions, Q, K, stream)
+    if st != RACE_OK:
+        raise RaceAttnError(st, "race_qk_rotary_fwd")
+    return Q, K
+
+
+def race_qk_rotary_bwd(desc: RaceRotaryDesc, q, k, wq, wk, inv_freq: Sequence[float], positions, dQ, dK, dq=None, dk=None, dwq=None, dwk=None,
+                       workspace=None, stream=None):
+    """Returns dq, dk in the layout (B, N, heads, d) (views with strides of their own if given) and dwq, dwk (None without weights)."""
+    torch = _torch()
+    keys = desc.Hk > 0
+    dq = torch.empty((desc.B, desc.N, desc.Hq, desc.d), dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty((desc.B, desc.N, desc.Hk, desc.d), dtype=k.dtype, device=k.device) if dk is None and keys else dk
+    dwq = torch.empty_like(wq) if dwq is None and wq is not None else dwq
+    dwk = torch.empty_like(wk) if dwk is None and wk is not None and keys else dwk
+    if workspace is None and (dwq is not None or dwk is not None):
+        workspace = _scratch(race_qk_rotary_workspace_bytes(desc), q.device)
+    st = (_native_module or _native()).rotary_bwd(desc, q, k, wq, wk, inv_freq, positions, dQ, dK, dq, dk, dwq, dwk, workspace, stream)
+    if st != RACE_OK:
+        raise RaceAttnError(st, "race_qk_rotary_bwd")
+    return dq, dk, dwq, dwk

@@ -1,0 +1,275 @@
+// What the kernels of the gated delta rule share: operands of the matrix instructions for both element types, the layouts of
+// tiles in LDS and in the workspace, and the arguments of the kernels.
+//
+// Mathematics.  Per value head, with decay a_t = exp(g_t) and write strength b_t,
+//     S_t = a_t S_{t-1} + k_t u_t^T,   u_t = b_t (v_t - a_t S_{t-1}^T k_t),   o_t = scale S_t^T q_t.
+// A chunk of C = 64 tokens that starts from S, with G_i the running sum of g inside the chunk and D_ij = exp(G_i - G_j), is
+//     (I + A) U = b (V - e^G K S),  A_ij = b_i D_ij k_i.k_j (j < i):   U = T b (V - e^G K S),  T = (I + A)^-1
+//     O = scale e^G Q S + M U,      M_ij = scale D_ij q_i.k_j (j <= i)
+//     S' = e^{G_C} S + (e^{G_C - G} K)^T U.
+// T, M and the decays of all chunks are formed at once (prep); only the products with S are one after the other.  S' is affine
+// in S, so a long sequence is cut into segments whose transition P and state from zero B are formed side by side (pre-pass),
+// joined (combine), and the pass proper then runs over all segments at once from their true states.
+//
+// Gradients, with dS the cotangent of the state behind the chunk:
+//     dU = M^T dO + e^{G_C - G} K dS,   dR = T^T dU,   dV = b dR,   dS' = e^{G_C} dS + (scale e^G Q)^T dO - (b e^G K)^T dR
+//     F_ij = scale D_ij dO_i.u_j (j <= i),   E_ij = -b_i D_ij dR_i.u_j (j < i)
+//     dQ = F K + scale e^G dO S^T
+//     dK = F^T Q + (E + E^T) K + e^{G_C - G} U dS^T - b e^G dR S^T
+//     db_i = u_i.dR_i / b_i
+//     dG_i = q_i.dQ_i - v_i.dV_i,   dg_t = sum_{i >= t, in the chunk} dG_i + <S', dS>
+// The last line: with S_t = e^{G_t} Z_t the recurrence of Z holds no decay, only v_t e^{-G_t} and o_t e^{G_t} do, so the cotangent of
+// G_t is o_t.dO_t - v_t.dV_t, and o is linear in q; a chunk's sum starts from the inner product at its end, which
+// keeps rounding errors from adding up along the sequence.  db divides by b: tokens with b = 0 are computed with b = 1e-18
+// throughout, far below any rounding, and u_i / b_i is then their error row to full precision.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace race {
+namespace delta {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+// a caller's rows need be aligned to their elements only; global memory takes wide accesses at any address
+typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any2;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any4;
+
+constexpr int C = 64;               // tokens per chunk
+constexpr float kBetaFloor = 1e-18f;
+constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 0 either way, and -infinity would make differences NaN
+
+// Element types.  An operand of a 16-deep product is 8 values a lane: lane l holds row (or column) l % 32 and, with h = l / 32,
+// the k of its 8 values: 8 h + 0..7 ("natural") or 8 a + 4 h + r, a = 0, 1, r = 0..3 ("spread": the rows that the lane holds of a
+// 32 x 32 accumulator's 16-row half, so that a product's result is the next product's operand without leaving the registers).
+// Any order will do, as long as both operands have it.
+//
+// bf16: v_mfma_f32_32x32x16_bf16.  The elements of Q, K, V and dO are exact as they are.  Values that are fp32 by their nature enter as
+// sums of bf16: three (Split: all 24 bits) where fp32 outputs (state, dg, db) hang on them, two (Pair: off by at most 2^-16) where
+// outputs of the element type alone do.  One bf16 (2^-8) would leave the fp32 outputs three digits; with two of them throughout dg was 1.5e-5 off at dk = 16.
+// The matrix instructions of the additional products are not what bounds any of the kernels.
+// fp32: eight v_mfma_f32_32x32x2_f32.
+struct Bf {
+    typedef uint16_t E;
+    typedef bf16x8 Exact;
+    struct Pair { bf16x8 hi, lo; };
+    struct Split { bf16x8 hi, mid, lo; };
+    static constexpr int kPlanes = 3, kPairPlanes = 2;      // of E for a value kept as a Split, as a Pair
+    static constexpr int kPad = 8;          // elements behind a row of a tile in LDS: 16 bytes, so that 8 rows lie in 8 places
+};
+struct Fp {
+    typedef float E;
+    struct Exact { float v[8]; };
+    typedef Exact Pair;
+    typedef Exact Split;
+    static constexpr int kPlanes = 1, kPairPlanes = 1;
+    static constexpr int kPad = 4;
+};
+
+__device__ __forceinline__ f32x16 zero16()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// the smallest terms first; terms below 2^-24 of the product are left out
+__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Exact &b, f32x16 c) { return mfma(a, b, c); }
+__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Pair &b, f32x16 c) { return mfma(a, b.hi, mfma(a, b.lo, c)); }
+__device__ __forceinline__ f32x16 mma(const Bf::Pair &a, const Bf::Exact &b, f32x16 c) { return mfma(a.hi, b, mfma(a.lo, b, c)); }
+__device__ __forceinline__ f32x16 mma(const Bf::Pair &a, const Bf::Pair &b, f32x16 c) { return mfma(a.hi, b.hi, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))); }
+__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Split &b, f32x16 c) { return mfma(a, b.hi, mfma(a, b.mid, mfma(a, b.lo, c))); }
+__device__ __forceinline__ f32x16 mma(const Bf::Split &a, const Bf::Exact &b, f32x16 c) { return mfma(a.hi, b, mfma(a.mid, b, mfma(a.lo, b, c))); }
+__device__ __forceinline__ f32x16 mma(const Bf::Split &a, const Bf::Split &b, f32x16 c)
+{
+    return mfma(a.hi, b.hi, mfma(a.hi, b.mid, mfma(a.mid, b.hi, mfma(a.mid, b.mid, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))))));
+}
+__device__ __forceinline__ Bf::Pair lead(const Bf::Split &a) { return Bf::Pair{a.hi, a.mid}; }
+__device__ __forceinline__ const Fp::Exact &lead(const Fp::Exact &a) { return a; }
+__device__ __forceinline__ f32x16 mma(const Fp::Exact &a, const Fp::Exact &b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+
+// 8 fp32 values as an operand
+__device__ __forceinline__ void split8(const float *x, Bf::Split &s)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const __bf16 hi = static_cast<__bf16>(x[j]);
+        const float rest = x[j] - static_cast<float>(hi);
+        const __bf16 mid = static_cast<__bf16>(rest);
+        s.hi[j] = hi;
+        s.mid[j] = mid;
+        s.lo[j] = static_cast<__bf16>(rest - static_cast<float>(mid));
+    }
+}
+__device__ __forceinline__ void split8(const float *x, Bf::Pair &s)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const __bf16 hi = static_cast<__bf16>(x[j]);
+        s.hi[j] = hi;
+        s.lo[j] = static_cast<__bf16>(x[j] - static_cast<float>(hi));
+    }
+}
+__device__ __forceinline__ void split8(const float *x, Fp::Exact &s)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s.v[j] = x[j];
+}
+__device__ __forceinline__ void round8(const float *x, Bf::Exact &s)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = static_cast<__bf16>(x[j]);
+}
+__device__ __forceinline__ void round8(const float *x, Fp::Exact &s) { split8(x, s); }
+
+// an operand from / to 8 elements that lie together, 16-byte aligned (LDS, workspace)
+__device__ __forceinline__ Bf::Exact get8(const uint16_t *p) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p)); }
+__device__ __forceinline__ Fp::Exact get8(const float *p)
+{
+    const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+    return Fp::Exact{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+__device__ __forceinline__ void put8(uint16_t *p, const Bf::Exact &x) { *reinterpret_cast<u32x4 *>(p) = __builtin_bit_cast(u32x4, x); }
+__device__ __forceinline__ void put8(float *p, const Fp::Exact &x)
+{
+    reinterpret_cast<f32x4 *>(p)[0] = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
+    reinterpret_cast<f32x4 *>(p)[1] = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
+}
+// a Split or a Pair lies in planes that are `plane` elements apart
+__device__ __forceinline__ void get8(const uint16_t *p, int plane, Bf::Split &x) { x = Bf::Split{get8(p), get8(p + plane), get8(p + 2 * plane)}; }
+__device__ __forceinline__ void get8(const uint16_t *p, int plane, Bf::Pair &x) { x = Bf::Pair{get8(p), get8(p + plane)}; }
+__device__ __forceinline__ void get8(const float *p, int, Fp::Exact &x) { x = get8(p); }
+__device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Split &x) { put8(p, x.hi); put8(p + plane, x.mid); put8(p + 2 * plane, x.lo); }
+__device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Pair &x) { put8(p, x.hi); put8(p + plane, x.lo); }
+__device__ __forceinline__ void put8(float *p, int, const Fp::Exact &x) { put8(p, x); }
+
+// one value
+__device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ void put1(uint16_t *p, float x) { *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
+__device__ __forceinline__ void put1(float *p, float x) { *p = x; }
+__device__ __forceinline__ void put1_pair(uint16_t *p, int plane, float x)
+{
+    const __bf16 hi = static_cast<__bf16>(x);
+    p[0] = __builtin_bit_cast(uint16_t, hi);
+    p[plane] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x - static_cast<float>(hi)));
+}
+__device__ __forceinline__ void put1_pair(float *p, int, float x) { *p = x; }
+__device__ __forceinline__ void values8(const Bf::Exact &x, float *f)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(x[j]);
+}
+__device__ __forceinline__ void values8(const Fp::Exact &x, float *f)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = x.v[j];
+}
+
+// 8 elements of a caller's row; zeros where there is none
+__device__ __forceinline__ Bf::Exact load8(const uint16_t *p, bool there)
+{
+    u32x4 v = {0, 0, 0, 0};
+    if (there) v = *reinterpret_cast<const u32x4_any2 *>(p);
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ Fp::Exact load8(const float *p, bool there)
+{
+    Fp::Exact x = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+    if (there) {
+        const f32x4 a = reinterpret_cast<const f32x4_any4 *>(p)[0], b = reinterpret_cast<const f32x4_any4 *>(p)[1];
+        x = Fp::Exact{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+    }
+    return x;
+}
+
+// The unit matrix as a right operand, 16 rows from 16 b of a 32 x 32 one.  A product with it turns an operand whose lanes hold rows into
+// an accumulator whose lanes hold columns, exactly (every value times one, plus zeros): rows that lie together in memory become
+// accumulators, and accumulators rows that are stored 8 or 16 bytes at a time, without a way through LDS.
+template <class X, bool SPREAD>
+__device__ __forceinline__ typename X::Exact unit8(int b, int lane)
+{
+    float x[8];
+    typename X::Exact u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int k = SPREAD ? 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3) : 8 * (lane >> 5) + j;
+        x[j] = 16 * b + k == (lane & 31) ? 1.f : 0.f;
+    }
+    round8(x, u);
+    return u;
+}
+
+// fp32 values at 4-byte aligned addresses; out of range (an offset of kNowhere too): zero, and not written
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+constexpr int kNowhere = -2147483647 - 1;
+__device__ __forceinline__ buffer_t buffer(const float *p, size_t floats)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, static_cast<int>(floats * sizeof(float)), 0x00020000);
+}
+__device__ __forceinline__ float get_buffer(buffer_t b, int offset) { return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0)); }
+__device__ __forceinline__ void put_buffer(buffer_t b, int offset, float x) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), b, offset, 0, 0); }
+
+// four elements of a caller's row
+__device__ __forceinline__ void store4(uint16_t *p, const float *x)
+{
+    typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any2;
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const __bf16 a = static_cast<__bf16>(x[2 * i]), b = static_cast<__bf16>(x[2 * i + 1]);
+        w[i] = __builtin_bit_cast(uint16_t, a) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, b)) << 16;
+    }
+    *reinterpret_cast<u32x2_any2 *>(p) = u32x2_any2{w[0], w[1]};
+}
+__device__ __forceinline__ void store4(float *p, const float *x) { *reinterpret_cast<f32x4_any4 *>(p) = f32x4_any4{x[0], x[1], x[2], x[3]}; }
+
+// 8 elements of a caller's row of which a lane takes two runs of four, 8 elements apart (spread order)
+__device__ __forceinline__ Bf::Exact load8_spread(const uint16_t *p, bool first, bool second)
+{
+    typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any2;
+    u32x2 a = {0, 0}, b = {0, 0};
+    if (first) a = *reinterpret_cast<const u32x2_any2 *>(p);
+    if (second) b = *reinterpret_cast<const u32x2_any2 *>(p + 8);
+    return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+}
+__device__ __forceinline__ Fp::Exact load8_spread(const float *p, bool first, bool second)
+{
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = {0.f, 0.f, 0.f, 0.f};
+    if (first) a = *reinterpret_cast<const f32x4_any4 *>(p);
+    if (second) b = *reinterpret_cast<const f32x4_any4 *>(p + 8);
+    return Fp::Exact{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+
+// place of k within a row that is stored in spread order
+__device__ __forceinline__ int spread(int k) { return (k & ~15) | ((k & 4) << 1) | ((k & 8) >> 1) | (k & 3); }
+// row of accumulator register i (32 x 32), within the tile
+__device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+__device__ __forceinline__ float gate(float g) { return g < kGateFloor ? kGateFloor : g; }       // NaN stays
+__device__ __forceinline__ float strength(float b) { return fabsf(b) < kBetaFloor ? kBetaFloor : b; }
+
+// running sum over the 64 lanes
+__device__ __forceinline__ double prefix64(double x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const double y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+}  // namespace delta
+}  // namespace race

@@ -1,0 +1,1253 @@
+// The gated delta rule: forward and backward pass over chunks of 64 tokens, and the decoding step.  The mathematics and the
+// operand layouts stand in delta_common.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "delta_common.h"
+#include "delta_plan.h"
+#include "internal.h"
+
+namespace race {
+namespace delta {
+namespace {
+
+struct Sizes {
+    int64_t N;
+    int H, Hk, dk, dv, dvp;         // dvp: dv rounded up to 32
+    float scale;
+    int seg_chunks, nseg;           // chunks per segment, segments of the sequence
+    int seg0, segs;                 // the window: first segment, segments
+    int chunk0, chunks;             // first chunk, chunks
+};
+
+__device__ __forceinline__ int64_t qk_row(const Sizes &z, int bh, int64_t t)
+{
+    const int b = bh / z.H, h = bh - b * z.H;
+    return (static_cast<int64_t>(b) * z.Hk + h / (z.H / z.Hk)) * z.N + t;
+}
+__device__ __forceinline__ int tokens_of(const Sizes &z, int chunk) { return static_cast<int>(min(static_cast<int64_t>(C), z.N - static_cast<int64_t>(chunk) * C)); }
+
+// one 32-row operand of caller's rows: row0 + lane % 32, elements k0 .. k0 + 7
+template <class X>
+__device__ __forceinline__ typename X::Exact rows8(const typename X::E *p, int row, int rows, int width, int k0)
+{
+    return load8(p + static_cast<int64_t>(row) * width + k0, row < rows && k0 < width);
+}
+
+// 8 values of an fp32 image
+__device__ __forceinline__ void kept8(const float *p, float *x)
+{
+    const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+}
+template <class OPERAND>
+__device__ __forceinline__ OPERAND kept(const float *p)
+{
+    float x[8];
+    OPERAND s;
+    kept8(p, x);
+    split8(x, s);
+    return s;
+}
+
+__device__ __forceinline__ void keep8(float *p, const float *x)
+{
+    reinterpret_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+    reinterpret_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+// ------------------------------------------------------------------ what a chunk needs besides the states
+// T, M and the decays of one chunk of one head.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane per
+// column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions.  Substitution and not powers of A: with keys alike the powers
+// reach thousands where T stays near one.
+// Images are written in the order in which the scans' operands lie in LDS (rows in spread order).
+template <int SIZE>
+__device__ __forceinline__ void merge_blocks(float (*A)[68], float (*T)[68], int base, int slab, int lane)
+{
+    const int r16 = lane & 15, q = lane >> 4;
+    constexpr int NT = SIZE / 16;
+    f32x4 P[NT];
+#pragma unroll
+    for (int ti = 0; ti < NT; ++ti) {
+        P[ti] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < SIZE / 4; ++k)
+            P[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[base + SIZE + 16 * ti + r16][base + 4 * k + q], T[base + 4 * k + q][base + 16 * slab + r16],
+                                                         P[ti], 0, 0, 0);
+    }
+#pragma unroll
+    for (int ti = 0; ti < NT; ++ti) {
+        f32x4 R = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int tk = 0; tk < NT; ++tk)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                R = __builtin_amdgcn_mfma_f32_16x16x4f32(T[base + SIZE + 16 * ti + r16][base + SIZE + 16 * tk + 4 * q + r], P[tk][r], R, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) T[base + SIZE + 16 * ti + 4 * q + r][base + 16 * slab + r16] = -R[r];
+    }
+}
+
+struct PrepArgs {
+    Sizes z;
+    const void *Q, *K;
+    const float *g, *beta;
+    float *T, *M;           // 64 x 64 each, rows in spread order; backward: also T^T, and M^T in M's place
+    float *TT;
+    float *dec;             // per chunk: e^G, e^{G_C - G}, beta
+};
+
+template <class X, int DK, bool BWD>
+__global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
+{
+    typedef typename X::E E;
+    __shared__ double G[C];
+    __shared__ float B[C];
+    __shared__ __attribute__((aligned(16))) float A[C][68], T[C][68];
+    const Sizes &z = a.z;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int bh = blockIdx.y, n = tokens_of(z, z.chunk0 + blockIdx.x);
+    const int64_t t0 = static_cast<int64_t>(z.chunk0 + blockIdx.x) * C;
+    const size_t at = static_cast<size_t>(bh) * z.chunks + blockIdx.x;
+    if (wave == 3) {
+        const int64_t t = static_cast<int64_t>(bh) * z.N + t0 + lane;
+        const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[t])) : 0.0, lane);
+        const float b = lane < n ? strength(a.beta[t]) : kBetaFloor;
+        G[lane] = g;
+        B[lane] = b;
+        float *dec = a.dec + at * 3 * C;
+        dec[lane] = expf(static_cast<float>(g));
+        dec[C + lane] = expf(static_cast<float>(__shfl(g, 63) - g));
+        dec[2 * C + lane] = b;
+    }
+    for (int i = tid; i < C * 68; i += 256) (&T[0][0])[i] = 0.f;
+    __syncthreads();
+    if (wave < 3) {
+        const int ti = wave > 0 ? 1 : 0, tj = wave == 2 ? 1 : 0;
+        const E *Q = static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, *K = static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk;
+        f32x16 kk = zero16(), qk = zero16();
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) {
+            const int k0 = 16 * kb + 8 * h;
+            const typename X::Exact ki = rows8<X>(K, 32 * ti + col, n, z.dk, k0), qi = rows8<X>(Q, 32 * ti + col, n, z.dk, k0);
+            const typename X::Exact kj = rows8<X>(K, 32 * tj + col, n, z.dk, k0);
+            kk = mma(ki, kj, kk);
+            qk = BWD ? mma(qi, kj, qk) : mma(kj, qi, qk);       // the image's row is the accumulator's column
+        }
+        float *M = a.M + at * C * C;
+#pragma unroll
+        for (int g16 = 0; g16 < 2; ++g16) {
+            float m[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = acc_row(8 * g16 + e, h);
+                const int i = 32 * ti + (BWD ? row : col), j = 32 * tj + (BWD ? col : row);
+                m[e] = j <= i ? z.scale * expf(static_cast<float>(G[i] - G[j])) * qk[8 * g16 + e] : 0.f;
+            }
+            keep8(M + (BWD ? (32 * tj + col) * C + 32 * ti : (32 * ti + col) * C + 32 * tj) + 16 * g16 + 8 * h, m);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = 32 * ti + acc_row(e, h), j = 32 * tj + col;
+            A[i][j] = j < i ? B[i] * expf(static_cast<float>(G[i] - G[j])) * kk[e] : 0.f;
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const int b0 = (lane >> 4) * 16, c16 = lane & 15;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == c16 ? 1.f : 0.f;
+#pragma unroll
+            for (int j = 0; j < i; ++j) s -= A[b0 + i][b0 + j] * x[j];
+            x[i] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) T[b0 + i][b0 + c16] = x[i];
+    }
+    __syncthreads();
+    if (wave < 2) merge_blocks<16>(A, T, 32 * wave, 0, lane);
+    __syncthreads();
+    if (wave < 2) merge_blocks<32>(A, T, 0, wave, lane);
+    __syncthreads();
+    for (int task = tid; task < C * 8; task += 256) {
+        const int row = task >> 3, k0 = 16 * ((task >> 1) & 3), hh = task & 1;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = T[row][k0 + acc_row(e, hh)];
+        keep8(a.T + at * C * C + row * C + k0 + 8 * hh, x);
+        if (BWD) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = T[k0 + acc_row(e, hh)][row];
+            keep8(a.TT + at * C * C + row * C + k0 + 8 * hh, x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ tiles in LDS
+template <class X, int DK>
+struct Lds {
+    typedef typename X::E E;
+    static constexpr int kRow = DK + X::kPad;       // a token's row, spread over k
+    static constexpr int kTok = C + X::kPad;        // a row over tokens, in spread order
+    static constexpr int kByTokens = C * kRow, kByRows = DK * kTok, kSquare = C * kTok;
+};
+
+// 64 rows of a caller's tensor into LDS: as they are (rows), or transposed, or both
+template <class X, int DK, bool ROWS, bool COLS>
+__device__ __forceinline__ void stage_rows(const typename X::E *src, int n, int dk, typename X::E *rows, typename X::E *cols, int tid)
+{
+    typedef typename X::E E;
+    typedef Lds<X, DK> L;
+#pragma unroll
+    for (int task = tid; task < 2 * DK; task += 256) {
+        const int tq = task & 15, o = task >> 4;            // four tokens, eight elements
+        typename X::Exact x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = rows8<X>(src, 4 * tq + r, n, dk, 8 * o);
+        E e[4][8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) __builtin_memcpy(e[r], &x[r], sizeof e[r]);
+        if (ROWS) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    E *to = rows + (4 * tq + r) * L::kRow + 16 * (o >> 1) + 8 * q + 4 * (o & 1);
+                    __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), &e[r][4 * q], 4 * sizeof(E));
+                }
+        }
+        if (COLS) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                E v[4] = {e[0][k], e[1][k], e[2][k], e[3][k]};
+                E *to = cols + (8 * o + k) * L::kTok + 16 * (tq >> 2) + 8 * (tq & 1) + 4 * ((tq >> 1) & 1);
+                __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), v, 4 * sizeof(E));
+            }
+        }
+    }
+}
+
+// a 64 x 64 fp32 image of the workspace into LDS as an operand in planes
+template <class X, class OPERAND>
+__device__ __forceinline__ void stage_image(const float *src, typename X::E *dst, int tid)
+{
+    constexpr int kTok = C + X::kPad;
+#pragma unroll
+    for (int task = tid; task < C * C / 8; task += 256) put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, kept<OPERAND>(src + task * 8));
+}
+
+// operand from a tile in LDS: rows row0 + lane % 32, 16 k from k0
+template <class X, int STRIDE>
+__device__ __forceinline__ typename X::Exact tile8(const typename X::E *t, int row0, int k0, int lane)
+{
+    return get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5));
+}
+template <class OPERAND, int STRIDE, class E>
+__device__ __forceinline__ OPERAND tile8s(const E *t, int row0, int k0, int lane)
+{
+    OPERAND x;
+    get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5), C * STRIDE, x);
+    return x;
+}
+
+// 8 rows (one half of an accumulator) times a factor per row, as an operand
+template <class X>
+__device__ __forceinline__ typename X::Split scaled8(const f32x16 &c, int half16, const float *factor, int h)
+{
+    float x[8];
+    typename X::Split s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e] * factor[acc_row(8 * half16 + e, h)];
+    split8(x, s);
+    return s;
+}
+template <class X>
+__device__ __forceinline__ typename X::Split half8(const f32x16 &c, int half16)
+{
+    float x[8];
+    typename X::Split s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e];
+    split8(x, s);
+    return s;
+}
+
+template <class X>
+__device__ __forceinline__ typename X::Exact round8_of(const f32x16 &c, int half16)
+{
+    float x[8];
+    typename X::Exact s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e];
+    round8(x, s);
+    return s;
+}
+// 32 x 32 accumulator with rows and columns exchanged
+template <class X, class OPERAND>
+__device__ __forceinline__ f32x16 exchanged(const OPERAND &first, const OPERAND &second, int lane)
+{
+    return mma(first, unit8<X, true>(0, lane), mma(second, unit8<X, true>(1, lane), zero16()));
+}
+// accumulator of 32 rows of a caller's tensor: rows row0 + .., elements k0 .. k0 + 31 in its lanes
+template <class X>
+__device__ __forceinline__ f32x16 acc_rows(const typename X::E *p, int row0, int rows, int width, int k0, int lane)
+{
+    const int h = lane >> 5;
+    return mma(rows8<X>(p, row0 + (lane & 31), rows, width, k0 + 8 * h), unit8<X, false>(0, lane),
+               mma(rows8<X>(p, row0 + (lane & 31), rows, width, k0 + 16 + 8 * h), unit8<X, false>(1, lane), zero16()));
+}
+// the way back, rounded to the element type
+template <class X>
+__device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows, int width, int k0, const f32x16 &c, int lane)
+{
+    const f32x16 t = exchanged<X>(round8_of<X>(c, 0), round8_of<X>(c, 1), lane);
+    const int row = row0 + (lane & 31);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int k = k0 + 8 * q + 4 * (lane >> 5);
+        const float x[4] = {t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+        if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, x);
+    }
+}
+// rows of an image in the workspace, fp32 or in planes: row of the accumulator -> row of the image, its 32 columns in spread order from k0
+template <class X>
+__device__ __forceinline__ void keep_rows(float *p, int row0, int width, int k0, const f32x16 &c, int lane)
+{
+    const f32x16 t = exchanged<X>(half8<X>(c, 0), half8<X>(c, 1), lane);
+    float *to = p + (row0 + (lane & 31)) * width + k0 + 8 * (lane >> 5);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(to + 16 * (q >> 1) + 4 * (q & 1)) = f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+}
+template <class X>
+__device__ __forceinline__ void keep_planes(typename X::E *p, int plane, int row0, int width, int k0, const f32x16 &c, int lane)
+{
+    const f32x16 t = exchanged<X>(half8<X>(c, 0), half8<X>(c, 1), lane);
+#pragma unroll
+    for (int g16 = 0; g16 < 2; ++g16) put8(p + (row0 + (lane & 31)) * width + k0 + 16 * g16 + 8 * (lane >> 5), plane, half8<X>(t, g16));
+}
+
+// accumulator of 32 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written
+__device__ __forceinline__ int state_offset(int row, int dv, int col) { return col < dv ? 4 * (row * dv + col) : kNowhere; }
+template <int DK>
+__device__ __forceinline__ void get_state(f32x16 (&S)[DK / 32], const float *state, int dk, int dv, int col, int h)
+{
+    const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[t][e] = get_buffer(b, state_offset(32 * t + acc_row(e, h), dv, col));
+}
+template <int DK>
+__device__ __forceinline__ void put_state(const f32x16 (&S)[DK / 32], float *state, int dk, int dv, int col, int h)
+{
+    const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) put_buffer(b, state_offset(32 * t + acc_row(e, h), dv, col), S[t][e]);
+}
+
+// ------------------------------------------------------------------ the states, chunk after chunk
+// One workgroup per segment, head and four tiles of 32 columns of the state; a wavefront keeps its columns of the state in
+// accumulators from chunk to chunk (DK x 32 fp32), where they are at once the right operand of the products with K and Q.
+// Columns never meet, so wavefronts share the tiles in LDS and nothing else.
+enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's transition and state from zero; states and U for the backward pass
+
+struct ScanArgs {
+    Sizes z;
+    const void *Q, *K, *V;
+    const float *T, *M, *dec;
+    const float *start;             // state at the start of a segment, (dk, dv) fp32: start + bh * start_head + segment * dk * dv; null: zero
+    size_t start_head;
+    float *final_state;             // state behind the window's last segment (null: not wanted); kPre: behind every segment
+    size_t final_head;
+    void *O;
+    void *P, *PT;                   // kPre: the transition and its transpose (Splits), per segment
+    int transitions;                // kPre
+    float *S, *U;                   // kKeep: states at the chunks' starts and behind the last, and U, rows in spread order
+};
+
+template <class X, int DK, int MODE>
+__global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
+{
+    typedef typename X::E E;
+    typedef Lds<X, DK> L;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPlanes * L::kSquare;
+    E *Ms = Qs + L::kByTokens;
+    float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPairPlanes * L::kSquare : Qs);
+    const Sizes &z = a.z;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int bh = blockIdx.z, seg = blockIdx.y;
+    const int vtiles = z.dvp / 32, tile = blockIdx.x * 4 + wave;
+    const bool trans = MODE == kPre && tile >= vtiles;
+    const bool active = MODE == kPre ? tile < vtiles + (a.transitions ? DK / 32 : 0) : tile < vtiles;
+    const int vcol = 32 * tile + col;                   // column of V (or, less the tiles of V, of the transition)
+    const int c0 = (z.seg0 + seg) * z.seg_chunks - z.chunk0, c1 = min(c0 + z.seg_chunks, z.chunks);
+
+    f32x16 S[DK / 32];
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
+    if (trans) {
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[t][e] = 32 * t + acc_row(e, h) == vcol - z.dvp ? 1.f : 0.f;
+    } else if (a.start && active) {
+        get_state<DK>(S, a.start + bh * a.start_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
+    }
+    for (int c = c0; c < c1; ++c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        const int n = tokens_of(z, z.chunk0 + c);
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        __syncthreads();
+        stage_rows<X, DK, true, true>(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, Ks, Kt, tid);
+        stage_image<X, typename X::Split>(a.T + at * C * C, Ts, tid);
+        if (MODE == kOut) {
+            stage_rows<X, DK, true, false>(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, Qs, nullptr, tid);
+            stage_image<X, typename X::Pair>(a.M + at * C * C, Ms, tid);
+        }
+        if (tid < 3 * C) dec[tid] = a.dec[at * 3 * C + tid];
+        __syncthreads();
+        if (!active) continue;
+        const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
+        const E *V = static_cast<const E *>(a.V) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
+        if (MODE == kKeep) {
+            float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp;
+#pragma unroll
+            for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+        }
+        // K S, and Q S for the outputs
+        f32x16 R[2] = {zero16(), zero16()}, O[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) {
+            const typename X::Split s = half8<X>(S[kb >> 1], kb & 1);
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) {
+                R[ti] = mma(tile8<X, L::kRow>(Ks, 32 * ti, 16 * kb, lane), s, R[ti]);
+                if (MODE == kOut) O[ti] = mma(tile8<X, L::kRow>(Qs, 32 * ti, 16 * kb, lane), lead(s), O[ti]);
+            }
+        }
+        // b (V - e^G K S)
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) {
+            f32x16 v = zero16();
+            if (MODE != kPre || !trans) v = acc_rows<X>(V, 32 * ti, n, z.dv, 32 * tile, lane);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = 32 * ti + acc_row(e, h);
+                R[ti][e] = beta[i] * (v[e] - eG[i] * R[ti][e]);
+                if (MODE == kOut) O[ti][e] *= z.scale * eG[i];
+            }
+        }
+        // U = T R, and the outputs' M U
+        f32x16 U[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const typename X::Split r = half8<X>(R[kb >> 1], kb & 1);
+#pragma unroll
+            for (int ti = kb >> 1; ti < 2; ++ti) U[ti] = mma(tile8s<typename X::Split, L::kTok>(Ts, 32 * ti, 16 * kb, lane), r, U[ti]);
+        }
+        if (MODE == kOut) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const typename X::Split u = half8<X>(U[kb >> 1], kb & 1);
+#pragma unroll
+                for (int ti = kb >> 1; ti < 2; ++ti) O[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ms, 32 * ti, 16 * kb, lane), lead(u), O[ti]);
+            }
+            E *out = static_cast<E *>(a.O) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) store_rows<X>(out, 32 * ti, n, z.dv, 32 * tile, O[ti], lane);
+        }
+        if (MODE == kKeep) {
+            float *keep = a.U + at * C * z.dvp;
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) keep_rows<X>(keep, 32 * ti, z.dvp, 32 * tile, U[ti], lane);
+        }
+        // the state behind the chunk
+        const float whole = eG[C - 1];
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[t][e] *= whole;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const typename X::Split u = scaled8<X>(U[kb >> 1], kb & 1, eEnd + 32 * (kb >> 1), h);
+#pragma unroll
+            for (int t = 0; t < DK / 32; ++t) S[t] = mma(tile8<X, L::kTok>(Kt, 32 * t, 16 * kb, lane), u, S[t]);
+        }
+    }
+    if (!active) return;
+    if (MODE == kKeep && c1 == z.chunks) {
+        float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+    }
+    if (trans) {
+        E *P = static_cast<E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
+        E *PT = static_cast<E *>(a.PT) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
+        const int k = vcol - z.dvp;
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t) {
+            keep_planes<X>(P, DK * DK, 32 * t, DK, 32 * tile - z.dvp, S[t], lane);
+#pragma unroll
+            for (int g16 = 0; g16 < 2; ++g16) put8(PT + k * DK + 32 * t + 16 * g16 + 8 * h, DK * DK, half8<X>(S[t], g16));
+        }
+        return;
+    }
+    if (a.final_state && (MODE == kPre || seg == z.segs - 1))
+        put_state<DK>(S, a.final_state + bh * a.final_head + (MODE == kPre ? static_cast<size_t>(seg) * z.dk * z.dv : 0), z.dk, z.dv, vcol, h);
+}
+
+// ------------------------------------------------------------------ states at the segments' starts
+// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T), one wavefront per head and 32 columns.
+struct CombineArgs {
+    Sizes z;
+    const float *carry;             // state to start from (null: zero): carry + bh * carry_head
+    size_t carry_head;
+    const void *P;
+    const float *add;               // B_s: add + (bh * nseg + s) * dk * dv
+    float *at;                      // states at the segments' starts (REV: cotangents at their ends), same layout, nseg + 1 (REV: nseg) of them a head
+    size_t at_head;
+    int steps;                      // transitions taken: segments seg0 .. seg0 + steps - 1 (REV: seg0 + segs - 1 down)
+};
+
+template <class X, int DK, bool REV>
+__global__ __launch_bounds__(64) void delta_combine_kernel(CombineArgs a)
+{
+    typedef typename X::E E;
+    const Sizes &z = a.z;
+    const int lane = threadIdx.x, h = lane >> 5, col = 32 * blockIdx.x + (lane & 31), bh = blockIdx.y;
+    const size_t one = static_cast<size_t>(z.dk) * z.dv;
+    f32x16 S[DK / 32];
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
+    if (a.carry) get_state<DK>(S, a.carry + bh * a.carry_head, z.dk, z.dv, col, h);
+    for (int i = 0; i <= a.steps; ++i) {
+        const int s = REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i;
+        put_state<DK>(S, a.at + bh * a.at_head + s * one, z.dk, z.dv, col, h);
+        if (i == a.steps) break;
+        const E *P = static_cast<const E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + s) * X::kPlanes * DK * DK;
+        f32x16 R[DK / 32];
+        get_state<DK>(R, a.add + (static_cast<size_t>(bh) * z.nseg + s) * one, z.dk, z.dv, col, h);
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) {
+            const typename X::Split x = half8<X>(S[kb >> 1], kb & 1);
+#pragma unroll
+            for (int t = 0; t < DK / 32; ++t) {
+                typename X::Split p;
+                get8(P + (32 * t + (lane & 31)) * DK + 16 * kb + 8 * h, DK * DK, p);
+                R[t] = mma(p, x, R[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t) S[t] = R[t];
+    }
+}
+
+// ------------------------------------------------------------------ cotangents of the states, last chunk first
+struct RevArgs {
+    Sizes z;
+    const void *Q, *K, *dO;
+    const float *TT, *MT, *dec;
+    const float *end;               // cotangent at the end of a segment: end + bh * end_head + segment * dk * dv (segment from the window's first); null: zero
+    size_t end_head;
+    float *final_state;             // cotangent of the state before the window's first segment; without FULL: before every segment (null: not wanted)
+    size_t final_head;
+    int seg_skip;                   // without FULL: segments of the window passed over
+    void *dV;
+    float *dS, *dR;                 // FULL: cotangents at the chunks' ends, and dR, rows in spread order
+};
+
+template <class X, int DK, bool FULL>
+__global__ __launch_bounds__(256) void delta_rev_kernel(RevArgs a)
+{
+    typedef typename X::E E;
+    typedef Lds<X, DK> L;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Qt = Kt + L::kByRows, *Ts = Qt + L::kByRows, *Ms = Ts + X::kPlanes * L::kSquare;
+    float *dec = reinterpret_cast<float *>(Ms + X::kPlanes * L::kSquare);
+    const Sizes &z = a.z;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5;
+    const int bh = blockIdx.z, seg = blockIdx.y + a.seg_skip;
+    const int tile = blockIdx.x * 4 + wave, vcol = 32 * tile + (lane & 31);
+    const bool active = tile < z.dvp / 32;
+    const int c0 = (z.seg0 + seg) * z.seg_chunks - z.chunk0, c1 = min(c0 + z.seg_chunks, z.chunks);
+
+    f32x16 S[DK / 32];
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
+    if (a.end && active) get_state<DK>(S, a.end + bh * a.end_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
+    for (int c = c1 - 1; c >= c0; --c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        const int n = tokens_of(z, z.chunk0 + c);
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        __syncthreads();
+        stage_rows<X, DK, true, true>(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, Ks, Kt, tid);
+        stage_rows<X, DK, false, true>(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, nullptr, Qt, tid);
+        stage_image<X, typename X::Split>(a.TT + at * C * C, Ts, tid);
+        stage_image<X, typename X::Split>(a.MT + at * C * C, Ms, tid);
+        if (tid < 3 * C) dec[tid] = a.dec[at * 3 * C + tid];
+        __syncthreads();
+        if (!active) continue;
+        const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
+        if (FULL) {
+            float *keep = a.dS + at * DK * z.dvp;
+#pragma unroll
+            for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+        }
+        const E *dO = static_cast<const E *>(a.dO) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
+        f32x16 d[2];
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) d[ti] = acc_rows<X>(dO, 32 * ti, n, z.dv, 32 * tile, lane);
+        // dU = M^T dO + e^{G_C - G} K dS
+        f32x16 U[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) {
+            const typename X::Split s = half8<X>(S[kb >> 1], kb & 1);
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) U[ti] = mma(tile8<X, L::kRow>(Ks, 32 * ti, 16 * kb, lane), s, U[ti]);
+        }
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) U[ti][e] *= eEnd[32 * ti + acc_row(e, h)];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const typename X::Exact o = round8_of<X>(d[kb >> 1], kb & 1);      // (exact: elements of dO)
+#pragma unroll
+            for (int ti = 0; ti <= kb >> 1; ++ti) U[ti] = mma(tile8s<typename X::Split, L::kTok>(Ms, 32 * ti, 16 * kb, lane), o, U[ti]);
+        }
+        // dR = T^T dU
+        f32x16 R[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const typename X::Split u = half8<X>(U[kb >> 1], kb & 1);
+#pragma unroll
+            for (int ti = 0; ti <= kb >> 1; ++ti) R[ti] = mma(tile8s<typename X::Split, L::kTok>(Ts, 32 * ti, 16 * kb, lane), u, R[ti]);
+        }
+        if (FULL) {
+            float *keep = a.dR + at * C * z.dvp;
+            E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) {
+                keep_rows<X>(keep, 32 * ti, z.dvp, 32 * tile, R[ti], lane);
+                f32x16 v;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = beta[32 * ti + acc_row(e, h)] * R[ti][e];
+                store_rows<X>(dV, 32 * ti, n, z.dv, 32 * tile, v, lane);
+            }
+        }
+        // the cotangent before the chunk
+        const float whole = eG[C - 1];
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[t][e] *= whole;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            float x[8], y[8];
+            typename X::Split o, r;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 32 * (kb >> 1) + acc_row(8 * (kb & 1) + e, h);
+                x[e] = z.scale * eG[i] * d[kb >> 1][8 * (kb & 1) + e];
+                y[e] = -beta[i] * eG[i] * R[kb >> 1][8 * (kb & 1) + e];
+            }
+            split8(x, o);
+            split8(y, r);
+#pragma unroll
+            for (int t = 0; t < DK / 32; ++t) {
+                S[t] = mma(tile8<X, L::kTok>(Qt, 32 * t, 16 * kb, lane), o, S[t]);
+                S[t] = mma(tile8<X, L::kTok>(Kt, 32 * t, 16 * kb, lane), r, S[t]);
+            }
+        }
+    }
+    if (active && a.final_state && (!FULL || seg == 0))
+        put_state<DK>(S, a.final_state + bh * a.final_head + (FULL ? 0 : static_cast<size_t>(seg) * z.dk * z.dv), z.dk, z.dv, vcol, h);
+}
+
+// ------------------------------------------------------------------ gradients of a chunk
+struct GradArgs {
+    Sizes z;
+    const void *Q, *K, *V, *dO;
+    const float *g, *beta;
+    const float *S, *U, *dS, *dR;
+    void *dQ, *dK;                  // the caller's tensors, or with `shared` fp32 (BH, 64 chunks, dk) parts
+    int shared;
+    float *dg, *dbeta;
+};
+
+// sums over the 32 lanes of a half of 32 values a lane: afterwards lane l holds the sum of value sum32_index(l)
+__device__ __forceinline__ float sum32(float (&v)[32], int lane)
+{
+#pragma unroll
+    for (int m = 16; m >= 1; m /= 2) {
+        const bool up = lane & m;
+#pragma unroll
+        for (int k = 0; k < m; ++k) {
+            const float keep = up ? v[k + m] : v[k], give = up ? v[k] : v[k + m];
+            v[k] = keep + __shfl_xor(give, m);
+        }
+    }
+    return v[0];
+}
+__device__ __forceinline__ int sum32_index(int lane) { return lane & 31; }
+
+// rows row0 + lane % 32 of a caller's tensor, 16 elements from k0 in spread order
+template <class X>
+__device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *p, int row, int rows, int width, int k0, int h)
+{
+    const int k = k0 + 4 * h;
+    return load8_spread(p + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 8 < width);
+}
+
+template <class X, int DK>
+__global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
+{
+    typedef typename X::E E;
+    typedef Lds<X, DK> L;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    double *G = reinterpret_cast<double *>(lds_raw);
+    float *eG = reinterpret_cast<float *>(G + C), *eEnd = eG + C, *bs = eEnd + C, *qd = bs + C /* 4 C */, *vd = qd + 4 * C, *part = vd + C /* 8 */;
+    E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *F = Qt + L::kByRows, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
+    const Sizes &z = a.z;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int bh = blockIdx.y, c = blockIdx.x, n = tokens_of(z, z.chunk0 + c);
+    const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
+    const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+    const E *K = static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, *Q = static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk;
+    const E *V = static_cast<const E *>(a.V) + row0 * z.dv, *dO = static_cast<const E *>(a.dO) + row0 * z.dv;
+    const float *S = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, *dS = a.dS + at * DK * z.dvp;
+    const float *U = a.U + at * C * z.dvp, *dR = a.dR + at * C * z.dvp;
+
+    if (wave == 3) {
+        const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[row0 + lane])) : 0.0, lane);
+        G[lane] = g;
+        eG[lane] = expf(static_cast<float>(g));
+        eEnd[lane] = expf(static_cast<float>(__shfl(g, 63) - g));
+        bs[lane] = lane < n ? strength(a.beta[row0 + lane]) : kBetaFloor;
+    }
+    qd[tid] = 0.f;
+    stage_rows<X, DK, false, true>(K, n, z.dk, nullptr, Kt, tid);
+    stage_rows<X, DK, false, true>(Q, n, z.dk, nullptr, Qt, tid);
+    __syncthreads();
+
+    // per token: u.dR and v.dV; over the states <S', dS>
+    {
+        const int i = tid >> 2;
+        float ud = 0.f, vr = 0.f;
+        for (int o = tid & 3; o < z.dvp / 8; o += 4) {
+            float u[8], r[8], v[8];
+            kept8(U + i * z.dvp + 8 * o, u);
+            kept8(dR + i * z.dvp + 8 * o, r);
+            values8(rows8_spread<X>(V, i, n, z.dv, 16 * (o >> 1), o & 1), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ud += u[e] * r[e];
+                vr += v[e] * r[e];
+            }
+        }
+        ud += __shfl_xor(ud, 1);
+        vr += __shfl_xor(vr, 1);
+        ud += __shfl_xor(ud, 2);
+        vr += __shfl_xor(vr, 2);
+        if ((tid & 3) == 0) {
+            vd[i] = bs[i] * vr;
+            if (i < n) a.dbeta[row0 + i] = ud / bs[i];
+        }
+        const float *S1 = S + DK * z.dvp;
+        float dot = 0.f;
+        for (int o = tid; o < DK * z.dvp / 8; o += 256) {
+            float x[8], y[8];
+            kept8(S1 + 8 * o, x);
+            kept8(dS + 8 * o, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
+        if (lane == 0) part[wave] = dot;
+    }
+    // F, its transpose, and E + E^T
+    if (wave < 3) {
+        const int ti = wave > 0 ? 1 : 0, tj = wave == 2 ? 1 : 0;
+        f32x16 zz = zero16(), xx = zero16();         // rows j, columns i
+        for (int kb = 0; kb < z.dvp / 16; ++kb) {
+            const int k0 = 16 * kb + 8 * h;
+            const typename X::Split uj = kept<typename X::Split>(U + (32 * tj + col) * z.dvp + k0);
+            zz = mma(uj, rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb, h), zz);
+            xx = mma(lead(uj), kept<typename X::Pair>(dR + (32 * ti + col) * z.dvp + k0), xx);
+        }
+        const int i = 32 * ti + col;
+#pragma unroll
+        for (int g16 = 0; g16 < 2; ++g16) {
+            float f[8], e8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = 32 * tj + acc_row(8 * g16 + e, h);
+                const float D = j <= i ? expf(static_cast<float>(G[i] - G[j])) : 0.f;
+                f[e] = z.scale * D * zz[8 * g16 + e];
+                e8[e] = j < i ? -bs[i] * D * xx[8 * g16 + e] : 0.f;
+                if (j > i) f[e] = 0.f;
+            }
+            typename X::Split s;
+            split8(f, s);
+            put8(F + i * L::kTok + 32 * tj + 16 * g16 + 8 * h, L::kSquare, s);
+            typename X::Pair x;
+            split8(e8, x);
+            put8(Es + i * L::kTok + 32 * tj + 16 * g16 + 8 * h, L::kSquare, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = 32 * tj + acc_row(8 * g16 + e, h);
+                put1_pair(Ft + j * L::kTok + spread(i), L::kSquare, f[e]);
+            }
+        }
+        // after the rows: in a diagonal tile these places hold its zeros
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int j = 32 * tj + acc_row(e, h);
+            if (j < i) put1_pair(Es + j * L::kTok + spread(i), L::kSquare, -bs[i] * expf(static_cast<float>(G[i] - G[j])) * xx[e]);
+        }
+    }
+    __syncthreads();
+    for (int task = wave; task < DK / 16; task += 4) {
+        const bool isq = task < DK / 32;
+        const int d0 = 32 * (isq ? task : task - DK / 32), dcol = d0 + col;
+        f32x16 R[2] = {zero16(), zero16()};
+        if (isq) {
+            for (int kb = 0; kb < z.dvp / 16; ++kb) {
+                const int k0 = 16 * kb + 8 * h;
+                const typename X::Split s = kept<typename X::Split>(S + dcol * z.dvp + k0);
+#pragma unroll
+                for (int ti = 0; ti < 2; ++ti) R[ti] = mma(rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb, h), s, R[ti]);
+            }
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) R[ti][e] *= z.scale * eG[32 * ti + acc_row(e, h)];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const typename X::Exact k = tile8<X, L::kTok>(Kt, d0, 16 * kb, lane);
+#pragma unroll
+                for (int ti = kb >> 1; ti < 2; ++ti) R[ti] = mma(tile8s<typename X::Split, L::kTok>(F, 32 * ti, 16 * kb, lane), k, R[ti]);
+            }
+            float p[32];
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+                for (int g16 = 0; g16 < 2; ++g16) {
+                    float q[8];
+                    values8(tile8<X, L::kTok>(Qt, d0, 32 * ti + 16 * g16, lane), q);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[16 * ti + 8 * g16 + e] = q[e] * R[ti][8 * g16 + e];
+                }
+            const float s = sum32(p, lane);
+            const int v = sum32_index(lane);
+            qd[wave * C + 32 * (v >> 4) + acc_row(v & 15, h)] += s;
+        } else {
+            f32x16 Y[2] = {zero16(), zero16()};
+            for (int kb = 0; kb < z.dvp / 16; ++kb) {
+                const int k0 = 16 * kb + 8 * h;
+                const typename X::Pair ds = kept<typename X::Pair>(dS + dcol * z.dvp + k0), s = kept<typename X::Pair>(S + dcol * z.dvp + k0);
+#pragma unroll
+                for (int ti = 0; ti < 2; ++ti) {
+                    R[ti] = mma(kept<typename X::Pair>(U + (32 * ti + col) * z.dvp + k0), ds, R[ti]);
+                    Y[ti] = mma(kept<typename X::Pair>(dR + (32 * ti + col) * z.dvp + k0), s, Y[ti]);
+                }
+            }
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int i = 32 * ti + acc_row(e, h);
+                    R[ti][e] = eEnd[i] * R[ti][e] - bs[i] * eG[i] * Y[ti][e];
+                }
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const typename X::Exact k = tile8<X, L::kTok>(Kt, d0, 16 * kb, lane), q = tile8<X, L::kTok>(Qt, d0, 16 * kb, lane);
+#pragma unroll
+                for (int ti = 0; ti < 2; ++ti) {
+                    R[ti] = mma(tile8s<typename X::Pair, L::kTok>(Es, 32 * ti, 16 * kb, lane), k, R[ti]);
+                    if (ti <= kb >> 1) R[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ft, 32 * ti, 16 * kb, lane), q, R[ti]);
+                }
+            }
+        }
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) {
+            if (!a.shared) {
+                store_rows<X>(static_cast<E *>(isq ? a.dQ : a.dK) + qk_row(z, bh, t0) * z.dk, 32 * ti, n, z.dk, d0, R[ti], lane);
+                continue;
+            }
+            const buffer_t out = buffer(static_cast<float *>(isq ? a.dQ : a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) put_buffer(out, state_offset(32 * ti + acc_row(e, h), z.dk, dcol), R[ti][e]);
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const float mine = qd[lane] + qd[C + lane] + qd[2 * C + lane] + qd[3 * C + lane] - vd[lane];
+        float s = mine;         // sum over this token and those behind it
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float y = __shfl_down(s, d);
+            if (lane + d < 64) s += y;
+        }
+        if (lane < n) a.dg[row0 + lane] = s + (part[0] + part[1] + part[2] + part[3]);
+    }
+}
+
+// dQ and dK of heads that value heads share: the parts in order
+template <class X>
+__global__ __launch_bounds__(256) void delta_shared_heads_kernel(Sizes z, int rows, const float *pq, const float *pk, void *dQ, void *dK)
+{
+    typedef typename X::E E;
+    const int bhk = blockIdx.y, group = z.H / z.Hk;
+    const int b = bhk / z.Hk, hk = bhk - b * z.Hk;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= static_cast<int64_t>(rows) * z.dk) return;
+    const size_t head = static_cast<size_t>(z.chunks) * C * z.dk;
+    const size_t from = (static_cast<size_t>(b) * z.H + static_cast<size_t>(hk) * group) * head + i;
+    float q = 0.f, k = 0.f;
+    for (int j = 0; j < group; ++j) {
+        q += pq[from + j * head];
+        k += pk[from + j * head];
+    }
+    const size_t to = (static_cast<size_t>(bhk) * z.N + static_cast<int64_t>(z.chunk0) * C) * z.dk + i;
+    put1(static_cast<E *>(dQ) + to, q);
+    put1(static_cast<E *>(dK) + to, k);
+}
+
+// ------------------------------------------------------------------ one token
+// The state is read and written once and everything else is small.  A workgroup owns 32 columns of one head's state: 8 lanes of four
+// columns by 32 groups of rows, four rows a lane (dk = 128), all held in registers between the two sums over rows.
+template <class E>
+__global__ __launch_bounds__(256) void delta_step_kernel(Sizes z, const E *q, const E *k, const E *v, const float *g, const float *beta, float *state, E *o)
+{
+    __shared__ float ks[128], qs[128];
+    __shared__ f32x4 sum[4][8];
+    const int tid = threadIdx.x, bh = blockIdx.y, c4 = tid & 7, rg = tid >> 3;
+    const int c0 = blockIdx.x * 32 + 4 * c4;
+    const bool there = c0 < z.dv;
+    const int64_t row = qk_row(z, bh, 0) * z.dk;
+    float *S = state + static_cast<size_t>(bh) * z.dk * z.dv + c0;
+    f32x4 s[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = rg + 32 * r;
+        s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (there && i < z.dk) s[r] = *reinterpret_cast<const f32x4_any4 *>(S + static_cast<size_t>(i) * z.dv);
+    }
+    if (tid < 128) {
+        ks[tid] = tid < z.dk ? value(k[row + tid]) : 0.f;
+        qs[tid] = tid < z.dk ? value(q[row + tid]) : 0.f;
+    }
+    const float a = expf(gate(g[bh])), b = beta[bh];
+    __syncthreads();
+    // sum over rows: the eight row groups of a wavefront, then the four wavefronts
+    auto over_rows = [&](const float *w) {
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t += s[r] * w[rg + 32 * r];
+#pragma unroll
+        for (int m = 8; m < 64; m *= 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += __shfl_xor(t[e], m);
+        __syncthreads();
+        if ((tid & 63) < 8) sum[tid >> 6][c4] = t;
+        __syncthreads();
+        return sum[0][c4] + sum[1][c4] + sum[2][c4] + sum[3][c4];
+    };
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] *= a;
+    f32x4 u = over_rows(ks);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = there ? b * (value(v[static_cast<size_t>(bh) * z.dv + c0 + e]) - u[e]) : 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = rg + 32 * r;
+        s[r] += u * ks[i];
+        if (there && i < z.dk) *reinterpret_cast<f32x4_any4 *>(S + static_cast<size_t>(i) * z.dv) = s[r];
+    }
+    const f32x4 out = over_rows(qs);
+    if (there && rg == 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put1(o + static_cast<size_t>(bh) * z.dv + c0 + e, z.scale * out[e]);
+}
+
+// ------------------------------------------------------------------ launches
+template <class X, int DK>
+constexpr size_t scan_lds(bool out)
+{
+    typedef Lds<X, DK> L;
+    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + 3 * C * sizeof(float);
+}
+template <class X, int DK>
+constexpr size_t rev_lds()
+{
+    typedef Lds<X, DK> L;
+    return sizeof(typename X::E) * (L::kByTokens + 2 * L::kByRows + 2 * X::kPlanes * L::kSquare) + 3 * C * sizeof(float);
+}
+template <class X, int DK>
+constexpr size_t grad_lds()
+{
+    typedef Lds<X, DK> L;
+    return sizeof(typename X::E) * (2 * L::kByRows + (X::kPlanes + 2 * X::kPairPlanes) * L::kSquare) + C * sizeof(double) + (8 * C + 8) * sizeof(float);
+}
+
+float *floats(char *ws, size_t at) { return reinterpret_cast<float *>(ws + at); }
+
+Sizes sizes_of(const DeltaPlan &p)
+{
+    Sizes z{};
+    z.N = p.N;
+    z.H = p.H;
+    z.Hk = p.Hk;
+    z.dk = p.dk;
+    z.dv = p.dv;
+    z.dvp = p.dvp;
+    z.scale = p.scale;
+    z.seg_chunks = p.seg_chunks;
+    z.nseg = p.nseg;
+    return z;
+}
+void set_window(const DeltaPlan &p, int w, Sizes *z)
+{
+    z->seg0 = w * p.win_segs;
+    z->segs = std::min(p.win_segs, p.nseg - z->seg0);
+    z->chunk0 = z->seg0 * p.seg_chunks;
+    z->chunks = std::min(z->segs * p.seg_chunks, p.chunks - z->chunk0);
+}
+
+#define DELTA_LAUNCH(name, kernel, grid, block, lds, st, ...)                                   \
+    do {                                                                                        \
+        ProfileScope scope(name, st);                                                           \
+        if (hipError_t e = allow_lds(kernel, lds); e != hipSuccess) return e;                   \
+        kernel<<<grid, block, lds, st>>>(__VA_ARGS__);                                          \
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;                        \
+    } while (0)
+
+template <class X, int DK>
+struct Passes {
+    static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
+    {
+        PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), floats(ws, p.off_M), bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
+        const dim3 grid(z.chunks, p.BH);
+        if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
+        else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
+        return hipSuccess;
+    }
+    static ScanArgs scan_args(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws)
+    {
+        ScanArgs a{};
+        a.z = z;
+        a.Q = io.Q;
+        a.K = io.K;
+        a.V = io.V;
+        a.T = floats(ws, p.off_T);
+        a.M = floats(ws, p.off_M);
+        a.dec = floats(ws, p.off_dec);
+        return a;
+    }
+    // transitions and states from zero of `segs` segments of the window
+    static hipError_t pre(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, int segs, hipStream_t st)
+    {
+        if (segs <= 0) return hipSuccess;
+        ScanArgs a = scan_args(p, z, io, ws);
+        const size_t one = static_cast<size_t>(p.dk) * p.dv;
+        a.final_state = floats(ws, p.off_add) + z.seg0 * one;
+        a.final_head = one * p.nseg;
+        a.transitions = 1;
+        a.P = ws + p.off_P;
+        a.PT = ws + p.off_PT;
+        const dim3 grid((p.dvp / 32 + DK / 32 + 3) / 4, segs, p.BH);
+        DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, kPre>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+        return hipSuccess;
+    }
+    static hipError_t combine(const DeltaPlan &p, const Sizes &z, const float *carry, size_t carry_head, char *ws, int steps, bool rev, hipStream_t st)
+    {
+        CombineArgs a{};
+        a.z = z;
+        a.carry = carry;
+        a.carry_head = carry_head;
+        a.P = ws + (rev ? p.off_PT : p.off_P);
+        a.add = floats(ws, p.off_add);
+        a.at = floats(ws, rev ? p.off_end : p.off_start);
+        a.at_head = static_cast<size_t>(p.dk) * p.dv * (rev ? p.nseg : p.nseg + 1);
+        a.steps = steps;
+        const dim3 grid(p.dvp / 32, p.BH);
+        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 64, 0, st, a);
+        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 64, 0, st, a);
+        return hipSuccess;
+    }
+
+    static hipError_t forward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st)
+    {
+        Sizes z = sizes_of(p);
+        const size_t one = static_cast<size_t>(p.dk) * p.dv;
+        const float *carry = io.state_in;
+        float *kept = floats(ws, p.off_carry);
+        for (int w = 0; w < p.windows; ++w) {
+            set_window(p, w, &z);
+            if (hipError_t e = prep(p, z, io, ws, false, st); e != hipSuccess) return e;
+            ScanArgs a = scan_args(p, z, io, ws);
+            a.O = io.O;
+            a.start = carry;
+            a.start_head = one;
+            if (z.segs > 1) {
+                if (hipError_t e = pre(p, z, io, ws, z.segs - 1, st); e != hipSuccess) return e;
+                if (hipError_t e = combine(p, z, carry, one, ws, z.segs - 1, false, st); e != hipSuccess) return e;
+                a.start = floats(ws, p.off_start) + z.seg0 * one;
+                a.start_head = one * (p.nseg + 1);
+            }
+            a.final_state = w + 1 < p.windows ? kept : io.state_out;
+            a.final_head = one;
+            carry = kept;
+            const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
+            DELTA_LAUNCH("delta_scan", (delta_scan_kernel<X, DK, kOut>), grid, 256, (scan_lds<X, DK>(true)), st, a);
+        }
+        return hipSuccess;
+    }
+
+    static hipError_t backward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st)
+    {
+        Sizes z = sizes_of(p);
+        const size_t one = static_cast<size_t>(p.dk) * p.dv;
+        float *start = floats(ws, p.off_start), *end = floats(ws, p.off_end);
+        const bool joined = p.win_segs > 1;
+        // states at the segments' starts
+        const float *carry = io.state_in;
+        for (int w = 0; w < p.windows; ++w) {
+            set_window(p, w, &z);
+            if (hipError_t e = prep(p, z, io, ws, true, st); e != hipSuccess) return e;
+            if (joined) {
+                if (hipError_t e = pre(p, z, io, ws, z.segs, st); e != hipSuccess) return e;
+                // the windows' starts follow one another in `start`, so the next window's carry is read there
+                if (hipError_t e = combine(p, z, w == 0 ? io.state_in : start + z.seg0 * one, w == 0 ? one : one * (p.nseg + 1), ws, z.segs, false, st); e != hipSuccess)
+                    return e;
+            } else {
+                ScanArgs a = scan_args(p, z, io, ws);
+                a.start = carry;
+                a.start_head = w == 0 ? one : one * (p.nseg + 1);
+                a.final_state = start + (w + 1) * one;
+                a.final_head = one * (p.nseg + 1);
+                carry = a.final_state;
+                if (w + 1 < p.windows) {
+                    const dim3 grid((p.dvp / 32 + 3) / 4, 1, p.BH);
+                    DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, kPre>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+                }
+            }
+        }
+        const float *dcarry = io.dstate_out;
+        float *kept = floats(ws, p.off_carry);
+        for (int w = p.windows - 1; w >= 0; --w) {
+            set_window(p, w, &z);
+            if (w != p.windows - 1)
+                if (hipError_t e = prep(p, z, io, ws, true, st); e != hipSuccess) return e;
+            {
+                ScanArgs a = scan_args(p, z, io, ws);
+                const bool own_start = joined || w > 0;
+                a.start = own_start ? start + z.seg0 * one : io.state_in;
+                a.start_head = own_start ? one * (p.nseg + 1) : one;
+                a.S = floats(ws, p.off_S);
+                a.U = floats(ws, p.off_U);
+                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
+                DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, kKeep>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+            }
+            RevArgs r{};
+            r.z = z;
+            r.Q = io.Q;
+            r.K = io.K;
+            r.dO = io.dO;
+            r.TT = floats(ws, p.off_TT);
+            r.MT = floats(ws, p.off_M);
+            r.dec = floats(ws, p.off_dec);
+            RevArgs full = r;
+            full.end = dcarry;
+            full.end_head = one;
+            if (z.segs > 1) {
+                r.final_state = floats(ws, p.off_add) + z.seg0 * one;
+                r.final_head = one * p.nseg;
+                r.seg_skip = 1;
+                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs - 1, p.BH);
+                DELTA_LAUNCH("delta_segments_back", (delta_rev_kernel<X, DK, false>), grid, 256, (rev_lds<X, DK>()), st, r);
+                if (hipError_t e = combine(p, z, dcarry, one, ws, z.segs - 1, true, st); e != hipSuccess) return e;
+                full.end = end + z.seg0 * one;
+                full.end_head = one * p.nseg;
+            }
+            full.final_state = w > 0 ? kept : io.dstate_in;
+            full.final_head = one;
+            full.dV = io.dV;
+            full.dS = floats(ws, p.off_dS);
+            full.dR = floats(ws, p.off_dR);
+            dcarry = kept;
+            {
+                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
+                DELTA_LAUNCH("delta_scan_back", (delta_rev_kernel<X, DK, true>), grid, 256, (rev_lds<X, DK>()), st, full);
+            }
+            const float *a_S = floats(ws, p.off_S), *a_U = floats(ws, p.off_U);
+            const bool shared = p.H != p.Hk;
+            GradArgs g{z, io.Q, io.K, io.V, io.dO, io.g, io.beta, a_S, a_U, full.dS, full.dR,
+                       shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta};
+            DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3(z.chunks, p.BH), 256, (grad_lds<X, DK>()), st, g);
+            if (shared) {
+                const int rows = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(z.chunks) * C, p.N - static_cast<int64_t>(z.chunk0) * C));
+                const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(rows) * p.dk + 255) / 256), p.BH / p.H * p.Hk);
+                DELTA_LAUNCH("delta_shared_heads", (delta_shared_heads_kernel<X>), grid, 256, 0, st, z, rows, floats(ws, p.off_pq),
+                             floats(ws, p.off_pk), io.dQ, io.dK);
+            }
+        }
+        return hipSuccess;
+    }
+};
+
+template <class F>
+hipError_t for_shape(const DeltaPlan &p, F f)
+{
+    if (p.dtype == RACE_BF16) return p.dk <= 64 ? f(Passes<Bf, 64>()) : f(Passes<Bf, 128>());
+    return p.dk <= 64 ? f(Passes<Fp, 64>()) : f(Passes<Fp, 128>());
+}
+
+__global__ __launch_bounds__(256) void delta_copy_state_kernel(const float *from, float *to, size_t n)
+{
+    const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i < n) to[i] = from ? from[i] : 0.f;
+}
+
+}  // namespace
+
+hipError_t forward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st)
+{
+    return for_shape(p, [&](auto passes) { return passes.forward(p, io, ws, st); });
+}
+hipError_t backward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st)
+{
+    return for_shape(p, [&](auto passes) { return passes.backward(p, io, ws, st); });
+}
+hipError_t copy_state(const DeltaPlan &p, const float *from, float *to, hipStream_t st)
+{
+    if (from == to) return hipSuccess;
+    const size_t n = static_cast<size_t>(p.BH) * p.dk * p.dv;
+    delta_copy_state_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(from, to, n);
+    return hipGetLastError();
+}
+hipError_t step(const DeltaPlan &p, const DeltaIo &io, hipStream_t st)
+{
+    Sizes z = sizes_of(p);
+    z.N = 1;
+    const dim3 grid(p.dvp / 32, p.BH);
+    if (p.dtype == RACE_BF16)
+        DELTA_LAUNCH("delta_step", delta_step_kernel<uint16_t>, grid, 256, 0, st, z, static_cast<const uint16_t *>(io.Q), static_cast<const uint16_t *>(io.K),
+                     static_cast<const uint16_t *>(io.V), io.g, io.beta, io.state_out, static_cast<uint16_t *>(io.O));
+    else
+        DELTA_LAUNCH("delta_step", delta_step_kernel<float>, grid, 256, 0, st, z, static_cast<const float *>(io.Q), static_cast<const float *>(io.K),
+                     static_cast<const float *>(io.V), io.g, io.beta, io.state_out, static_cast<float *>(io.O));
+    return hipSuccess;
+}
+
+}  // namespace delta
+}  // namespace race

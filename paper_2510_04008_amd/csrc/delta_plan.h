@@ -1,0 +1,39 @@
+// Plan of a gated delta rule call: what the host side (operators_api.cpp) derives from a validated descriptor and the launches
+// (delta_kernels.hip) follow.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace race {
+namespace delta {
+
+struct DeltaPlan {
+    int B, H, Hk, BH, dk, dv, dvp, dtype;       // dvp: dv rounded up to 32
+    int64_t N;
+    float scale;
+    int chunks;                     // of 64 tokens
+    int seg_chunks, nseg;           // chunks per segment (the last may be short), segments
+    int win_segs, windows;          // segments per window (the last may hold fewer), windows: a window's workspace is the next one's too
+    // workspace, byte offsets (multiples of 256).  Per window: T, M (backward: M^T), decays and, backward, T^T, states, U, cotangents, dR
+    size_t off_T, off_M, off_dec, off_TT, off_S, off_U, off_dS, off_dR, off_pq, off_pk;
+    // per segment of the sequence: states (cotangents) from zero, transitions, states at the starts, cotangents at the ends
+    size_t off_add, off_P, off_PT, off_start, off_end;
+    size_t off_carry;               // one state a head between windows
+    size_t total;
+};
+
+struct DeltaIo {
+    const void *Q, *K, *V, *dO;
+    const float *g, *beta, *state_in, *dstate_out;
+    void *O, *dQ, *dK, *dV;
+    float *state_out, *dg, *dbeta, *dstate_in;
+};
+
+hipError_t forward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st);
+hipError_t backward(const DeltaPlan &p, const DeltaIo &io, char *ws, hipStream_t st);
+hipError_t step(const DeltaPlan &p, const DeltaIo &io, hipStream_t st);        // io.state_out is the state, updated in place
+hipError_t copy_state(const DeltaPlan &p, const float *from, float *to, hipStream_t st);       // from null: zeros
+
+}  // namespace delta
+}  // namespace race

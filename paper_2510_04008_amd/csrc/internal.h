@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "race_attn.h"
 
 namespace race {
@@ -84,6 +86,11 @@ constexpr size_t kStaticLimitBytes = static_cast<size_t>(32) << 20;
 hipError_t static_scratch(void **ptr);     // device address of the current device's copy
 // Host: plain (H, L*P, d) expansion into caller memory.
 void expand_projection_host(int H, int L, int P, int d, int dtype, const uint64_t *seeds, float *out);
+
+// Records the text behind RACE_ERR_HIP for race_attn_last_error and returns that status (race_api.cpp).
+race_status_t hip_failed(hipError_t e, const char *where);
+// Whether one of `outs` occurs more than once in `all` (an output given as another argument too).
+bool any_equal(std::initializer_list<const void *> outs, std::initializer_list<const void *> all);
 
 // Brackets one kernel launch with HIP events on its stream while profiling is enabled (benchmark aid).
 struct ProfileScope {

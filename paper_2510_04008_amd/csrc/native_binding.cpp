@@ -51,7 +51,7 @@ void *tensor(PyObject *o, const char *name, const Shape &shape, at::ScalarType t
     std::string want;
     for (int i = 0; i < shape.n; ++i) want += (i ? ", " : "") + std::to_string(shape.s[i]);
     PyErr_Format(PyExc_ValueError, "%s must be a contiguous device tensor of shape (%s) and dtype %s", name, want.c_str(),
-                 type == at::kFloat ? "torch.float32" : "torch.bfloat16");
+                 type == at::kFloat ? "torch.float32" : type == at::kLong ? "torch.int64" : "torch.bfloat16");
     throw BadArgument{};
 }
 Shape full(const Desc &d) { return Shape{4, {d.d.B, d.d.H, d.d.N, d.d.d}}; }
@@ -227,12 +227,216 @@ PyObject *step(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---------------------------------------------------------------- the gated delta rule, rows of queries and keys
+template <class D>
+D plain_desc(PyObject *o, const char *type)
+{
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw BadArgument{};
+    D d;
+    const bool ok = view.len == static_cast<Py_ssize_t>(sizeof d);
+    if (ok) std::memcpy(&d, view.buf, sizeof d);
+    PyBuffer_Release(&view);
+    if (!ok) {
+        PyErr_Format(PyExc_TypeError, "desc must be a %s", type);
+        throw BadArgument{};
+    }
+    return d;
+}
+at::ScalarType elem_of(int32_t dtype) { return dtype == RACE_F32 ? at::kFloat : at::kBFloat16; }
+
+// Tensors of one call: contiguous, of the current device (its stream is the one that they are used on).
+struct Call {
+    const int device = c10::hip::current_device();
+    void on_device(const at::Tensor &t, const char *name) const
+    {
+        if (t.get_device() == device) return;
+        PyErr_Format(PyExc_ValueError, "%s is on device %d, the current device is %d", name, static_cast<int>(t.get_device()), device);
+        throw BadArgument{};
+    }
+    void *operator()(PyObject *o, const char *name, const Shape &shape, at::ScalarType type) const
+    {
+        void *p = tensor(o, name, shape, type);
+        on_device(THPVariable_Unpack(o), name);
+        return p;
+    }
+    float *floats(PyObject *o, const char *name, const Shape &shape) const { return static_cast<float *>((*this)(o, name, shape, at::kFloat)); }
+    float *maybe(PyObject *o, const char *name, const Shape &shape) const { return o == Py_None ? nullptr : floats(o, name, shape); }
+    Workspace workspace(PyObject *o) const
+    {
+        const Workspace w(o);
+        if (o == Py_None) return w;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || !t.is_contiguous()) {
+            PyErr_SetString(PyExc_ValueError, "workspace must be a contiguous device tensor");
+            throw BadArgument{};
+        }
+        on_device(t, "workspace");
+        return w;
+    }
+    // rows (B, N, heads, d), the elements of a row together; their strides
+    void *rows(PyObject *o, const char *name, const Shape &shape, at::ScalarType type, int64_t *strides) const
+    {
+        if (THPVariable_Check(o)) {
+            const at::Tensor &t = THPVariable_Unpack(o);
+            bool ok = t.is_cuda() && t.scalar_type() == type && t.dim() == 4 && t.stride(3) == 1;
+            for (int i = 0; ok && i < 4; ++i) ok = t.size(i) == shape.s[i];
+            if (ok) {
+                on_device(t, name);
+                for (int i = 0; i < 3; ++i) strides[i] = t.stride(i);
+                return t.data_ptr();
+            }
+        }
+        PyErr_Format(PyExc_ValueError, "%s must be a device tensor of shape (%lld, %lld, %lld, %lld) and dtype %s with stride 1 in its last dimension", name,
+                     static_cast<long long>(shape.s[0]), static_cast<long long>(shape.s[1]), static_cast<long long>(shape.s[2]),
+                     static_cast<long long>(shape.s[3]), type == at::kFloat ? "torch.float32" : "torch.bfloat16");
+        throw BadArgument{};
+    }
+};
+
+struct DeltaShapes {
+    Shape qk, v, gates, state;
+    DeltaShapes(const race_delta_desc_t &d, bool step)
+    {
+        const int64_t B = d.B, H = d.H, Hk = d.Hk, N = d.N, dk = d.dk, dv = d.dv;
+        qk = step ? Shape{3, {B, Hk, dk}} : Shape{4, {B, Hk, N, dk}};
+        v = step ? Shape{3, {B, H, dv}} : Shape{4, {B, H, N, dv}};
+        gates = step ? Shape{2, {B, H}} : Shape{3, {B, H, N}};
+        state = Shape{4, {B, H, dk, dv}};
+    }
+};
+
+// (desc, Q, K, V, g, beta, state_in or None, O, state_out or None, workspace, stream)
+PyObject *delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return call<11>(args, n, [](PyObject *const *a) {
+        const auto d = plain_desc<race_delta_desc_t>(a[0], "RaceDeltaDesc");
+        const DeltaShapes s(d, false);
+        const at::ScalarType e = elem_of(d.dtype);
+        const Call t;
+        void *Q = t(a[1], "Q", s.qk, e), *K = t(a[2], "K", s.qk, e), *V = t(a[3], "V", s.v, e);
+        const float *g = t.floats(a[4], "g", s.gates), *beta = t.floats(a[5], "beta", s.gates), *in = t.maybe(a[6], "state_in", s.state);
+        void *O = t(a[7], "O", s.v, e);
+        float *out = t.maybe(a[8], "state_out", s.state);
+        const Workspace ws = t.workspace(a[9]);
+        const race_stream_t st = stream_of(a[10]);
+        const ReleaseGil released;
+        return race_delta_fwd(&d, Q, K, V, g, beta, in, O, out, ws.ptr, ws.bytes, st);
+    });
+}
+
+// (desc, Q, K, V, g, beta, state_in or None, dO, dstate_out or None, dQ, dK, dV, dg, dbeta, dstate_in or None, workspace, stream)
+PyObject *delta_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return call<17>(args, n, [](PyObject *const *a) {
+        const auto d = plain_desc<race_delta_desc_t>(a[0], "RaceDeltaDesc");
+        const DeltaShapes s(d, false);
+        const at::ScalarType e = elem_of(d.dtype);
+        const Call t;
+        void *Q = t(a[1], "Q", s.qk, e), *K = t(a[2], "K", s.qk, e), *V = t(a[3], "V", s.v, e);
+        const float *g = t.floats(a[4], "g", s.gates), *beta = t.floats(a[5], "beta", s.gates), *in = t.maybe(a[6], "state_in", s.state);
+        void *dO = t(a[7], "dO", s.v, e);
+        const float *dout = t.maybe(a[8], "dstate_out", s.state);
+        void *dQ = t(a[9], "dQ", s.qk, e), *dK = t(a[10], "dK", s.qk, e), *dV = t(a[11], "dV", s.v, e);
+        float *dg = t.floats(a[12], "dg", s.gates), *dbeta = t.floats(a[13], "dbeta", s.gates), *din = t.maybe(a[14], "dstate_in", s.state);
+        const Workspace ws = t.workspace(a[15]);
+        const race_stream_t st = stream_of(a[16]);
+        const ReleaseGil released;
+        return race_delta_bwd(&d, Q, K, V, g, beta, in, dO, dout, dQ, dK, dV, dg, dbeta, din, ws.ptr, ws.bytes, st);
+    });
+}
+
+// (desc, q, k, v, g, beta, state, o, stream)
+PyObject *delta_step(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return call<9>(args, n, [](PyObject *const *a) {
+        const auto d = plain_desc<race_delta_desc_t>(a[0], "RaceDeltaDesc");
+        const DeltaShapes s(d, true);
+        const at::ScalarType e = elem_of(d.dtype);
+        const Call t;
+        void *q = t(a[1], "q", s.qk, e), *k = t(a[2], "k", s.qk, e), *v = t(a[3], "v", s.v, e);
+        const float *g = t.floats(a[4], "g", s.gates), *beta = t.floats(a[5], "beta", s.gates);
+        float *state = t.floats(a[6], "state", s.state);
+        void *o = t(a[7], "o", s.v, e);
+        const race_stream_t st = stream_of(a[8]);
+        const ReleaseGil released;
+        return race_delta_step(&d, q, k, v, g, beta, state, o, st);
+    });
+}
+
+struct Rotary {
+    race_rotary_desc_t d;
+    const Call t;
+    at::ScalarType e;
+    const void *q, *k = nullptr;
+    const float *wq, *wk = nullptr;
+    double freq[128];
+    const int64_t *positions = nullptr;
+    // desc, q, k or None, wq or None, wk or None, inv_freq, positions or None
+    explicit Rotary(PyObject *const *a) : d(plain_desc<race_rotary_desc_t>(a[0], "RaceRotaryDesc")), e(elem_of(d.dtype))
+    {
+        q = t.rows(a[1], "q", given(d.Hq), e, d.q_strides);
+        wq = t.maybe(a[3], "wq", Shape{1, {d.d}});
+        if (d.Hk > 0) {
+            k = t.rows(a[2], "k", given(d.Hk), e, d.k_strides);
+            wk = t.maybe(a[4], "wk", Shape{1, {d.d}});
+        }
+        const Py_ssize_t need = d.rot / 2;
+        PyObject *fast = need > 0 ? PySequence_Fast(a[5], "inv_freq must be a sequence of numbers") : nullptr;
+        if (need > 0 && !fast) throw BadArgument{};
+        if (need > 128 || (need > 0 && PySequence_Fast_GET_SIZE(fast) != need)) {
+            Py_XDECREF(fast);
+            PyErr_Format(PyExc_ValueError, "inv_freq must have rot / 2 (%d) elements", static_cast<int>(need));
+            throw BadArgument{};
+        }
+        for (Py_ssize_t i = 0; i < need; ++i) freq[i] = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(fast, i));
+        Py_XDECREF(fast);
+        if (PyErr_Occurred()) throw BadArgument{};
+        if (a[6] != Py_None) positions = static_cast<const int64_t *>(t(a[6], "positions", Shape{2, {d.B, d.N}}, at::kLong));
+    }
+    Shape given(int64_t heads) const { return Shape{4, {d.B, d.N, heads, d.d}}; }
+    Shape made(int64_t heads) const { return Shape{4, {d.B, heads, d.N, d.d}}; }
+};
+
+// (desc, q, k, wq, wk, inv_freq, positions, Q, K or None, stream)
+PyObject *rotary_fwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return call<10>(args, n, [](PyObject *const *a) {
+        const Rotary r(a);
+        void *Q = r.t(a[7], "Q", r.made(r.d.Hq), r.e), *K = r.d.Hk > 0 ? r.t(a[8], "K", r.made(r.d.Hk), r.e) : nullptr;
+        const race_stream_t st = stream_of(a[9]);
+        const ReleaseGil released;
+        return race_qk_rotary_fwd(&r.d, r.q, r.k, r.wq, r.wk, r.freq, r.positions, Q, K, st);
+    });
+}
+
+// (desc, q, k, wq, wk, inv_freq, positions, dQ, dK or None, dq, dk or None, dwq or None, dwk or None, workspace or None, stream)
+PyObject *rotary_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return call<15>(args, n, [](PyObject *const *a) {
+        Rotary r(a);
+        const bool keys = r.d.Hk > 0;
+        void *dQ = r.t(a[7], "dQ", r.made(r.d.Hq), r.e), *dK = keys ? r.t(a[8], "dK", r.made(r.d.Hk), r.e) : nullptr;
+        void *dq = r.t.rows(a[9], "dq", r.given(r.d.Hq), r.e, r.d.dq_strides), *dk = keys ? r.t.rows(a[10], "dk", r.given(r.d.Hk), r.e, r.d.dk_strides) : nullptr;
+        float *dwq = r.t.maybe(a[11], "dwq", Shape{1, {r.d.d}}), *dwk = r.t.maybe(a[12], "dwk", Shape{1, {r.d.d}});
+        const Workspace ws = r.t.workspace(a[13]);
+        const race_stream_t st = stream_of(a[14]);
+        const ReleaseGil released;
+        return race_qk_rotary_bwd(&r.d, r.q, r.k, r.wq, r.wk, r.freq, r.positions, dQ, dK, dq, dk, dwq, dwk, ws.ptr, ws.bytes, st);
+    });
+}
+
 #define ENTRY(name, doc) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, doc}
 PyMethodDef kMethods[] = {
     ENTRY(fwd, "race_attn_fwd, or race_attn_fwd_static without a workspace"),
     ENTRY(bwd, "race_attn_bwd_beta or race_attn_bwd_saved"),
     ENTRY(state_init, "race_attn_state_init"),
     ENTRY(step, "race_attn_step"),
+    ENTRY(delta_fwd, "race_delta_fwd"),
+    ENTRY(delta_bwd, "race_delta_bwd"),
+    ENTRY(delta_step, "race_delta_step"),
+    ENTRY(rotary_fwd, "race_qk_rotary_fwd"),
+    ENTRY(rotary_bwd, "race_qk_rotary_bwd"),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the RACE Attention entry points", -1, kMethods,

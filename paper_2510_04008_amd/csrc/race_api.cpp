@@ -317,19 +317,10 @@ race_status_t make_plan(const race_attn_desc_t *desc, Plan *pl)
     return RACE_OK;
 }
 
-namespace {
-
 race_status_t hip_failed(hipError_t e, const char *where)
 {
     g_last_error = std::string(where) + ": " + hipGetErrorString(e);
     return RACE_ERR_HIP;
-}
-
-race_status_t check_workspace(const Plan &p, const void *ws, size_t bytes, size_t need)
-{
-    (void)p;
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || bytes < need) return RACE_ERR_WORKSPACE;
-    return RACE_OK;
 }
 
 bool any_equal(std::initializer_list<const void *> outs, std::initializer_list<const void *> all)
@@ -340,6 +331,15 @@ bool any_equal(std::initializer_list<const void *> outs, std::initializer_list<c
         if (hits > 1) return true;
     }
     return false;
+}
+
+namespace {
+
+race_status_t check_workspace(const Plan &p, const void *ws, size_t bytes, size_t need)
+{
+    (void)p;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || bytes < need) return RACE_ERR_WORKSPACE;
+    return RACE_OK;
 }
 
 // Copies the image of W to its place in the workspace (and zeroes `clear_bytes` at `clear` on the way).

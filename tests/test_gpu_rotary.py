@@ -1,0 +1,250 @@
+"""GPU tests of the rotated rows of queries and keys against fp64.
+
+Tolerances: arithmetic is fp32, a dozen roundings of 2^-24 behind one another and a sum over at most 256 elements; a row is rounded once more to bf16 (2^-8 of
+the value).  The weights' gradients sum all rows of the call in fp32: 2^-24 for each of the at most 1024 additions behind one another."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_04008_amd as ra
+from oracle import rotary as oracle
+
+pytestmark = pytest.mark.gpu
+
+ROWS = {"bf16": 2.0**-8, "f32": 2.0**-20}
+WEIGHTS = 2.0**-14
+TYPES = {"bf16": (torch.bfloat16, ra.RACE_BF16), "f32": (torch.float32, ra.RACE_F32)}
+
+
+def _freq(rot):
+    return [10000.0 ** (-2.0 * i / rot) for i in range(rot // 2)]
+
+
+def _inputs(B, N, Hq, Hk, d, dtype, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    t = TYPES[dtype][0]
+    x = {n: torch.randn(s, generator=gen).to(t) for n, s in (("q", (B, N, Hq, d)), ("k", (B, N, Hk, d)), ("dQ", (B, Hq, N, d)), ("dK", (B, Hk, N, d)))}
+    x.update({n: 1 + 0.3 * torch.randn(d, generator=gen) for n in ("wq", "wk")})
+    return x
+
+
+def _want(x, positions, freq, rot, norm, eps, pairs, weights=True):
+    out = {}
+    for n in ("q", "k"):
+        a = (x[n].double().numpy(), x["w" + n].double().numpy() if weights else None, positions, freq, rot, norm, eps, pairs == "neighbours")
+        out[n.upper()] = oracle.forward(*a)
+        out["d" + n], out["dw" + n] = oracle.backward(*a, x["d" + n.upper()].double().numpy())
+    return out
+
+
+def _check(got, want, dtype, label=""):
+    torch.cuda.synchronize()
+    for n, w in want.items():
+        x = got[n].double().cpu().numpy()
+        assert x.shape == w.shape and np.isfinite(x).all(), (label, n)
+        tol = WEIGHTS if n.startswith("dw") else ROWS[dtype]
+        off, norm = np.linalg.norm(x - w), np.linalg.norm(w)
+        print("%s %s: rel %.2e of %.2e" % (label, n, off / max(norm, 1e-30), tol), flush=True)
+        assert off <= tol * norm, (label, n, off / norm)
+        assert np.abs(x - w).max() <= 4 * tol * np.abs(w).max(), (label, n)
+
+
+def _run(x, desc, freq, positions, weights=True, **kw):
+    y = {n: v.cuda() for n, v in x.items()}
+    w = (y["wq"], y["wk"]) if weights else (None, None)
+    Q, K = ra.race_qk_rotary_fwd(desc, y["q"], y["k"], *w, freq, positions, **{n: kw[n] for n in ("Q", "K") if n in kw})
+    dq, dk, dwq, dwk = ra.race_qk_rotary_bwd(desc, y["q"], y["k"], *w, freq, positions, y["dQ"], y["dK"])
+    out = {"Q": Q, "K": K, "dq": dq, "dk": dk}
+    if weights:
+        out.update(dwq=dwq, dwk=dwk)
+    else:
+        assert dwq is None and dwk is None
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+@pytest.mark.parametrize("B,N,Hq,Hk,d,rot,norm", [
+    (1, 1, 1, 1, 8, 8, "rms"), (2, 3, 2, 1, 8, 2, "l2"), (1, 5, 3, 2, 16, 0, "rms"), (2, 33, 4, 4, 64, 64, "rms"), (1, 17, 2, 1, 80, 20, "none"),
+    (3, 7, 8, 2, 96, 64, "l2"), (1, 130, 2, 2, 128, 128, "rms"), (1, 9, 4, 1, 128, 32, "none"), (1, 3, 2, 2, 200, 100, "rms"), (2, 5, 1, 1, 256, 256, "l2"),
+    (1, 4, 2, 3, 256, 134, "rms"), (65, 1, 6, 2, 128, 128, "rms")])
+def test_passes(B, N, Hq, Hk, d, rot, norm, pairs, dtype):
+    x = _inputs(B, N, Hq, Hk, d, dtype, seed=d + N)
+    desc = ra.make_rotary_desc(B, N, Hq, Hk, d, rot, TYPES[dtype][1], norm=norm, pairs=pairs, eps=1e-3, pos0=11)
+    places = np.broadcast_to(11 + np.arange(N), (B, N))
+    _check(_run(x, desc, _freq(rot), None), _want(x, places, _freq(rot), rot, norm, np.float64(np.float32(1e-3)), pairs), dtype, "d%d rot%d %s" % (d, rot, norm))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_far_and_own_positions(dtype):
+    """Positions of each token's own, negative and beyond 2^31 among them; fp32 angles would be worthless there."""
+    B, N, d = 2, 50, 64
+    x = _inputs(B, N, 2, 1, d, dtype)
+    places = np.random.RandomState(0).randint(-1000, 12_000_000, (B, N)).astype(np.int64)
+    places[0, 0], places[1, 1] = 0, (1 << 32) + 12345
+    desc = ra.make_rotary_desc(B, N, 2, 1, d, d, TYPES[dtype][1])
+    got = _run(x, desc, _freq(d), torch.from_numpy(places).cuda())
+    _check(got, _want(x, places, _freq(d), d, "rms", np.float64(np.float32(1e-6)), "halves"), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_without_weights_and_without_keys(dtype):
+    x = _inputs(1, 20, 2, 2, 64, dtype)
+    desc = ra.make_rotary_desc(1, 20, 2, 2, 64, 64, TYPES[dtype][1], norm="l2")
+    places = np.arange(20)[None]
+    want = _want(x, places, _freq(64), 64, "l2", np.float64(np.float32(1e-6)), "halves", weights=False)
+    got = _run(x, desc, _freq(64), None, weights=False)
+    _check(got, {n: want[n] for n in ("Q", "K", "dq", "dk")}, dtype)
+    alone = ra.make_rotary_desc(1, 20, 2, 0, 64, 64, TYPES[dtype][1], norm="l2")
+    q, dQ = x["q"].cuda(), x["dQ"].cuda()
+    Q, K = ra.race_qk_rotary_fwd(alone, q, None, None, None, _freq(64))
+    dq, dk, dwq, dwk = ra.race_qk_rotary_bwd(alone, q, None, None, None, _freq(64), None, dQ, None)
+    assert K is None and dk is None and dwq is None and dwk is None
+    assert torch.equal(Q, got["Q"]) and torch.equal(dq, got["dq"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot", [(64, 64), (40, 20)])
+def test_views_of_a_fused_projection(dtype, d, rot):
+    """Rows and cotangents inside wider tensors, token-major and head-major, at odd element offsets: the same bits as contiguous rows, and nothing beside the
+    rows is written."""
+    B, N, Hq, Hk = 2, 37, 3, 2
+    x = _inputs(B, N, Hq, Hk, d, dtype)
+    t = TYPES[dtype][0]
+    desc = ra.make_rotary_desc(B, N, Hq, Hk, d, rot, TYPES[dtype][1])
+    want = _run(x, desc, _freq(rot), None)
+    y = {n: v.cuda() for n, v in x.items()}
+    width = (Hq + 2 * Hk) * d + 1
+
+    def views(buf):
+        rows = buf[1:1 + B * N * width].view(B, N, width)
+        return rows[..., :Hq * d].unflatten(-1, (Hq, d)), rows[..., Hq * d:(Hq + Hk) * d].unflatten(-1, (Hk, d)), rows[..., (Hq + Hk) * d:]
+
+    def heads_first(buf):
+        a, b = buf[:B * Hq * N * d].view(B, Hq, N, d).transpose(1, 2), buf[B * Hq * N * d:B * (Hq + Hk) * N * d].view(B, Hk, N, d).transpose(1, 2)
+        return a, b, buf[B * (Hq + Hk) * N * d:]
+
+    for of in (views, heads_first):
+        given, cot = (torch.full((1 + B * N * width,), 3.0, dtype=t, device="cuda") for _ in range(2))
+        q, k, _ = of(given)
+        q.copy_(y["q"]), k.copy_(y["k"])
+        dq, dk, rest = of(cot)
+        Q, K = ra.race_qk_rotary_fwd(desc, q, k, y["wq"], y["wk"], _freq(rot))
+        ra.race_qk_rotary_bwd(desc, q, k, y["wq"], y["wk"], _freq(rot), None, y["dQ"], y["dK"], dq=dq, dk=dk)
+        torch.cuda.synchronize()
+        for a, n in ((Q, "Q"), (K, "K"), (dq, "dq"), (dk, "dk")):
+            assert torch.equal(a, want[n]), n
+        assert (rest == 3).all()
+    # one row of keys for all heads
+    one = y["k"][:, :, :1].expand(B, N, Hk, d)
+    K1 = ra.race_qk_rotary_fwd(desc, y["q"], one, y["wq"], y["wk"], _freq(rot))[1]
+    assert torch.equal(K1[:, 0], K1[:, 1]) and torch.equal(K1[:, 0], want["K"][:, 0])
+
+
+def test_special_rows():
+    """Zero rows stay zero; a non-finite element spreads over its own row alone."""
+    x = _inputs(1, 12, 2, 2, 64, "f32")
+    desc = ra.make_rotary_desc(1, 12, 2, 2, 64, 64, ra.RACE_F32)
+    want = _run(x, desc, _freq(64), None)
+    x["q"][0, 3, 1], x["q"][0, 5, 0, 7], x["k"][0, 6, 1, 0] = 0.0, float("inf"), float("nan")
+    got = _run(x, desc, _freq(64), None)
+    assert (got["Q"][0, 1, 3] == 0).all() and torch.isfinite(got["dq"][0, 3, 1]).all()
+    for a, b, rows in (("Q", "Q", {(0, 5), (1, 3)}), ("K", "K", {(1, 6)})):
+        for h in range(2):
+            for n in range(12):
+                if (h, n) not in rows:
+                    assert torch.equal(got[a][0, h, n], want[b][0, h, n])
+
+
+def test_streams_and_graphs():
+    x = _inputs(2, 40, 4, 2, 128, "bf16")
+    desc = ra.make_rotary_desc(2, 40, 4, 2, 128, 128, ra.RACE_BF16)
+    y = {n: v.cuda() for n, v in x.items()}
+    places = torch.arange(80, device="cuda").view(2, 40) * 1000
+    out = {"Q": torch.empty_like(y["dQ"]), "K": torch.empty_like(y["dK"]), "dq": torch.empty_like(y["q"]), "dk": torch.empty_like(y["k"]),
+           "dwq": torch.empty_like(y["wq"]), "dwk": torch.empty_like(y["wk"])}
+    ws = torch.empty(ra.race_qk_rotary_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+
+    def run(stream=None):
+        ra.race_qk_rotary_fwd(desc, y["q"], y["k"], y["wq"], y["wk"], _freq(128), places, Q=out["Q"], K=out["K"], stream=stream)
+        ra.race_qk_rotary_bwd(desc, y["q"], y["k"], y["wq"], y["wk"], _freq(128), places, y["dQ"], y["dK"], dq=out["dq"], dk=out["dk"], dwq=out["dwq"],
+                              dwk=out["dwk"], workspace=ws, stream=stream)
+
+    run()
+    torch.cuda.synchronize()
+    want = {n: v.clone() for n, v in out.items()}
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    run(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n], want[n]) for n in want)
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for _ in range(3):
+        for v in out.values():
+            v.zero_()
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[n], want[n]) for n in want)
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[n], want[n]) for n in want)
+    # positions are read when the graph runs
+    places.add_(5)
+    run()
+    torch.cuda.synchronize()
+    want = {n: v.clone() for n, v in out.items()}
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n], want[n]) for n in want)
+
+
+def test_many_rows():
+    """More rows than partial sums of the weights' gradients, beyond 2^31 bytes of rows."""
+    B, N, Hq, Hk, d = 1, 530000, 8, 1, 256
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, dQ, dK = (torch.randn(s, generator=gen, device="cuda", dtype=torch.bfloat16) for s in ((B, N, Hq, d), (B, N, Hk, d), (B, Hq, N, d), (B, Hk, N, d)))
+    assert q.numel() * 2 > 1 << 31
+    wq, wk = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda") for _ in range(2))
+    desc = ra.make_rotary_desc(B, N, Hq, Hk, d, d, ra.RACE_BF16)
+    Q, K = ra.race_qk_rotary_fwd(desc, q, k, wq, wk, _freq(d))
+    dq, dk, dwq, dwk = ra.race_qk_rotary_bwd(desc, q, k, wq, wk, _freq(d), None, dQ, dK)
+    at = slice(N - 40, N)
+    x = {"q": q[:, at], "k": k[:, at], "dQ": dQ[:, :, at], "dK": dK[:, :, at], "wq": wq, "wk": wk}
+    want = _want({n: v.cpu() for n, v in x.items()}, np.arange(N - 40, N)[None], _freq(d), d, "rms", np.float64(np.float32(1e-6)), "halves")
+    _check({"Q": Q[:, :, at], "K": K[:, :, at], "dq": dq[:, at], "dk": dk[:, at]}, {n: want[n] for n in ("Q", "K", "dq", "dk")}, "bf16")
+    whole = [ra.race_qk_rotary_bwd(ra.make_rotary_desc(B, 10600, Hq, Hk, d, d, ra.RACE_BF16, pos0=a), q[:, a:a + 10600], k[:, a:a + 10600], wq, wk, _freq(d), None,
+                                   dQ[:, :, a:a + 10600].contiguous(), dK[:, :, a:a + 10600].contiguous())[2:] for a in range(0, N, 10600)]
+    for got, parts in ((dwq, [p[0] for p in whole]), (dwk, [p[1] for p in whole])):
+        want = torch.stack(parts).double().sum(0)
+        assert (got.double() - want).norm() <= 2 * WEIGHTS * want.norm()
+
+
+def test_every_tensor_is_checked():
+    x = {n: v.cuda() for n, v in _inputs(1, 10, 2, 1, 16, "f32").items()}
+    desc = ra.make_rotary_desc(1, 10, 2, 1, 16, 16, ra.RACE_F32)
+    f = _freq(16)
+    for n in ("q", "k", "wq", "wk"):
+        for w in (lambda t: t[..., :-1], lambda t: t.half(), lambda t: t.cpu(), lambda t: t.unsqueeze(0), lambda t: torch.stack((t, t), -1)[..., 0]):
+            y = dict(x)
+            y[n] = w(x[n])
+            with pytest.raises(ValueError):
+                ra.race_qk_rotary_fwd(desc, y["q"], y["k"], y["wq"], y["wk"], f)
+    for n in ("dQ", "dK"):
+        for w in (lambda t: t[..., :-1], lambda t: t.transpose(1, 2)):
+            y = dict(x)
+            y[n] = w(x[n])
+            with pytest.raises(ValueError):
+                ra.race_qk_rotary_bwd(desc, x["q"], x["k"], x["wq"], x["wk"], f, None, y["dQ"], y["dK"])
+    for bad in (f[:-1], f + [1.0], 3):
+        with pytest.raises((ValueError, TypeError)):
+            ra.race_qk_rotary_fwd(desc, x["q"], x["k"], x["wq"], x["wk"], bad)
+    for places in (torch.zeros(1, 10, device="cuda"), torch.zeros(10, dtype=torch.int64, device="cuda"), torch.zeros(1, 10, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            ra.race_qk_rotary_fwd(desc, x["q"], x["k"], x["wq"], x["wk"], f, places)
+    with pytest.raises(ra.RaceAttnError):
+        ra.race_qk_rotary_fwd(desc, x["q"], x["k"], x["wq"], x["wk"], f[:-1] + [float("nan")])
+    same = torch.empty(1, 10, 1, 16, device="cuda").expand(1, 10, 2, 16)
+    with pytest.raises(ra.RaceAttnError):
+        ra.race_qk_rotary_bwd(desc, x["q"], x["k"], x["wq"], x["wk"], f, None, x["dQ"], x["dK"], dq=same)

@@ -1,0 +1,177 @@
+"""CPU-only checks of the gated delta rule's and the rotated rows' C ABI: what is refused, before a device is touched."""
+import ctypes
+
+import pytest
+
+import paper_2510_04008_amd as ra
+
+
+def _p(i):
+    return ctypes.c_void_p(256 * (i + 1))
+
+
+def _delta(**kw):
+    base = dict(B=2, H=4, Hk=2, N=100, dk=64, dv=64, scale=0.125, dtype=ra.RACE_BF16, chunk=0)
+    base.update(kw)
+    return ra.make_delta_desc(**base)
+
+
+def _fwd(d, ws=_p(99), bytes_=1 << 40, skip=None, same=None):
+    """Pointers 0..7: Q, K, V, g, beta, state_in, O, state_out; `skip`: a null pointer, `same`: (i, j) given the same address."""
+    a = [_p(i) for i in range(8)]
+    if skip is not None:
+        a[skip] = None
+    if same:
+        a[same[0]] = a[same[1]]
+    return ra.lib().race_delta_fwd(ctypes.byref(d), *a, ws, bytes_, None)
+
+
+def _bwd(d, ws=_p(99), bytes_=1 << 40, skip=None, same=None):
+    """0..13: Q, K, V, g, beta, state_in, dO, dstate_out, dQ, dK, dV, dg, dbeta, dstate_in"""
+    a = [_p(i) for i in range(14)]
+    if skip is not None:
+        a[skip] = None
+    if same:
+        a[same[0]] = a[same[1]]
+    return ra.lib().race_delta_bwd(ctypes.byref(d), *a, ws, bytes_, None)
+
+
+BAD = [dict(B=0), dict(H=0), dict(Hk=0), dict(H=3), dict(Hk=8), dict(N=-1), dict(dk=0), dict(dv=-8), dict(scale=float("nan")), dict(scale=float("inf")),
+       dict(dtype=2), dict(chunk=-1)]
+UNBUILT = [dict(dk=12), dict(dv=20), dict(dk=136), dict(dv=136), dict(B=40000, H=2), dict(N=(1 << 36) + 1)]
+
+
+@pytest.mark.parametrize("bad,status", [(b, ra.RACE_ERR_INVALID_ARG) for b in BAD] + [(b, ra.RACE_ERR_UNSUPPORTED) for b in UNBUILT])
+def test_delta_descriptors(bad, status):
+    d = _delta(**bad)
+    assert _fwd(d) == status and _bwd(d) == status
+    assert ra.race_delta_workspace_bytes(d) == 0 and ra.race_delta_bwd_workspace_bytes(d) == 0 and ra.race_delta_segment_tokens(d) == 0
+    if not {"N", "chunk"} & set(bad):
+        assert ra.race_delta_state_bytes(d) == 0
+        assert ra.lib().race_delta_step(ctypes.byref(d), *[_p(i) for i in range(7)], None) == status
+
+
+def test_delta_pointers_and_workspace():
+    d = _delta()
+    need, back = ra.race_delta_workspace_bytes(d), ra.race_delta_bwd_workspace_bytes(d)
+    assert 0 < need < back and ra.race_delta_state_bytes(d) == 4 * 2 * 4 * 64 * 64
+    for i in (0, 1, 2, 3, 4, 6):
+        assert _fwd(d, skip=i) == ra.RACE_ERR_INVALID_ARG
+    for i in (0, 1, 2, 3, 4, 6, 8, 9, 10, 11, 12):
+        assert _bwd(d, skip=i) == ra.RACE_ERR_INVALID_ARG
+    for i in range(7):
+        a = [None if j == i else _p(j) for j in range(7)]
+        assert ra.lib().race_delta_step(ctypes.byref(d), *a, None) == ra.RACE_ERR_INVALID_ARG
+    for same in ((6, 0), (6, 2), (7, 2), (7, 6), (6, 5)):
+        assert _fwd(d, same=same) == ra.RACE_ERR_INVALID_ARG
+    for same in ((8, 0), (9, 8), (10, 6), (11, 3), (12, 11), (13, 5), (13, 8)):
+        assert _bwd(d, same=same) == ra.RACE_ERR_INVALID_ARG
+    for ws, n in ((None, 1 << 40), (ctypes.c_void_p(128), 1 << 40), (_p(99), need - 1)):
+        assert _fwd(d, ws, n) == ra.RACE_ERR_WORKSPACE
+    assert _bwd(d, _p(99), back - 1) == ra.RACE_ERR_WORKSPACE
+    empty = _delta(N=0)
+    assert ra.race_delta_workspace_bytes(empty) == 0 and _fwd(empty, skip=7) == ra.RACE_OK and _bwd(empty, skip=13) == ra.RACE_OK
+    assert ra.lib().race_delta_fwd(None, *[_p(i) for i in range(8)], _p(99), 1 << 40, None) == ra.RACE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("B,H,N", [(1, 1, 1), (1, 4, 65), (1, 4, 1 << 20), (8, 32, 5000), (64, 32, 100000)])
+def test_delta_segments_cover_the_sequence(B, H, N):
+    d = _delta(B=B, H=H, Hk=1, N=N)
+    n = ra.race_delta_segment_tokens(d)
+    assert n % 64 == 0 and 64 <= n < N + 64
+    for chunk in (1, 64, 65, 1000):
+        d = _delta(B=B, H=H, Hk=1, N=N, chunk=chunk)
+        assert ra.race_delta_segment_tokens(d) == min(-(-chunk // 64), -(-N // 64)) * 64
+
+
+def test_delta_workspace_is_bounded():
+    # beyond the first window only what a segment leaves behind grows
+    one, two = (ra.race_delta_bwd_workspace_bytes(_delta(B=1, H=4, N=n, dk=128, dv=128)) for n in (1 << 22, 1 << 23))
+    assert two - one < 2 * (1 << 30) and two < 16 << 30
+
+
+def _rotary(**kw):
+    base = dict(B=2, N=100, Hq=4, Hk=2, d=64, rot=64, dtype=ra.RACE_BF16)
+    strides = dict(q_strides=(25600, 256, 64), k_strides=(12800, 128, 64), dq_strides=(25600, 256, 64), dk_strides=(12800, 128, 64))
+    for n in list(kw):
+        if n in strides:
+            strides[n] = kw.pop(n)
+    fields = {n: kw.pop(n) for n in list(kw) if n in ("norm_", "neighbours_")}
+    base.update(kw)
+    d = ra.make_rotary_desc(**base)
+    for n, s in strides.items():
+        setattr(d, n, (ctypes.c_int64 * 3)(*s))
+    for n, v in fields.items():
+        setattr(d, n[:-1], v)
+    return d
+
+
+FREQ = (ctypes.c_double * 128)(*([1.0] * 128))
+
+
+def _rfwd(d, skip=None, same=None, freq=FREQ):
+    """q, k, wq, wk | positions, Q, K"""
+    a = [_p(i) for i in range(7)]
+    if skip is not None:
+        a[skip] = None
+    if same:
+        a[same[0]] = a[same[1]]
+    return ra.lib().race_qk_rotary_fwd(ctypes.byref(d), *a[:4], freq, *a[4:], None)
+
+
+def _rbwd(d, skip=None, same=None, ws=_p(99), bytes_=1 << 30, freq=FREQ):
+    """q, k, wq, wk | positions, dQ, dK, dq, dk, dwq, dwk"""
+    a = [_p(i) for i in range(11)]
+    if skip is not None:
+        a[skip] = None
+    if same:
+        a[same[0]] = a[same[1]]
+    return ra.lib().race_qk_rotary_bwd(ctypes.byref(d), *a[:4], freq, *a[4:], ws, bytes_, None)
+
+
+@pytest.mark.parametrize("bad,status", [(b, ra.RACE_ERR_INVALID_ARG) for b in (
+    dict(B=0), dict(Hq=0), dict(Hk=-1), dict(N=-1), dict(d=0), dict(rot=-2), dict(rot=33), dict(rot=66), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(eps=float("inf")), dict(dtype=5), dict(norm_=3), dict(norm_=-1), dict(neighbours_=2), dict(q_strides=(-1, 256, 64)), dict(dk_strides=(12800, 128, -64)))] +
+    [(b, ra.RACE_ERR_UNSUPPORTED) for b in (dict(d=60, rot=60), dict(d=264), dict(Hq=65536), dict(B=1 << 16, N=1 << 16))])
+def test_rotary_descriptors(bad, status):
+    d = _rotary(**bad)
+    assert _rfwd(d) == status and _rbwd(d) == status and ra.race_qk_rotary_workspace_bytes(d) == 0
+
+
+def test_rotary_pointers_and_workspace():
+    d = _rotary()
+    need = ra.race_qk_rotary_workspace_bytes(d)
+    assert need > 0
+    for i in (0, 1, 5, 6):
+        assert _rfwd(d, skip=i) == ra.RACE_ERR_INVALID_ARG
+    for i in (0, 1, 5, 6, 7, 8):
+        assert _rbwd(d, skip=i) == ra.RACE_ERR_INVALID_ARG
+    assert _rfwd(d, freq=None) == ra.RACE_ERR_INVALID_ARG and _rbwd(d, freq=None) == ra.RACE_ERR_INVALID_ARG
+    nan = (ctypes.c_double * 128)(*([1.0] * 5 + [float("nan")] * 123))
+    assert _rfwd(d, freq=nan) == ra.RACE_ERR_INVALID_ARG
+    for same in ((5, 0), (6, 5), (6, 1), (5, 2)):
+        assert _rfwd(d, same=same) == ra.RACE_ERR_INVALID_ARG
+    for same in ((7, 0), (8, 7), (9, 2), (10, 9), (8, 6)):
+        assert _rbwd(d, same=same) == ra.RACE_ERR_INVALID_ARG
+    for ws, n in ((None, 1 << 30), (ctypes.c_void_p(64), 1 << 30), (_p(99), need - 1)):
+        assert _rbwd(d, ws=ws, bytes_=n) == ra.RACE_ERR_WORKSPACE
+    # weights of keys that there are not
+    assert _rbwd(_rotary(Hk=0)) == ra.RACE_ERR_INVALID_ARG
+
+
+def test_rotary_cotangent_rows_must_not_overlap():
+    for strides in ((25600, 256, 32), (25600, 255, 64), (0, 256, 64), (256, 256, 64), (25600, 0, 64), (25536, 256, 64)):
+        assert _rbwd(_rotary(dq_strides=strides)) == ra.RACE_ERR_INVALID_ARG, strides
+    # any order of the axes, and gaps, are fine; a stride of an axis of one element says nothing
+    ok = [dict(dq_strides=(64, 512, 128)), dict(dq_strides=(25600, 64, 6400)), dict(B=1, dq_strides=(0, 256, 64), dk_strides=(0, 128, 64))]
+    for kw in ok:
+        assert _rbwd(_rotary(**kw), ws=None) == ra.RACE_ERR_WORKSPACE
+    # rows that are only read may be the same row
+    assert _rbwd(_rotary(q_strides=(0, 256, 0)), ws=None) == ra.RACE_ERR_WORKSPACE
+
+
+def test_names_of_options():
+    with pytest.raises(ValueError):
+        ra.make_rotary_desc(1, 1, 1, 1, 8, 8, ra.RACE_F32, norm="layer")
+    with pytest.raises(ValueError):
+        ra.make_rotary_desc(1, 1, 1, 1, 8, 8, ra.RACE_F32, pairs="odd")
