@@ -252,6 +252,21 @@ __device__ __forceinline__ Fp::Exact load8_spread(const float *p, bool first, bo
     return Fp::Exact{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
 
+__device__ __forceinline__ Bf::Exact or_zero(const Bf::Exact &x, bool there)
+{
+    u32x4 v = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = there ? v[i] : 0;
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ Fp::Exact or_zero(const Fp::Exact &x, bool there)
+{
+    Fp::Exact y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y.v[i] = there ? x.v[i] : 0.f;
+    return y;
+}
+
 // place of k within a row that is stored in spread order
 __device__ __forceinline__ int spread(int k) { return (k & ~15) | ((k & 4) << 1) | ((k & 8) >> 1) | (k & 3); }
 // row of accumulator register i (32 x 32), within the tile

@@ -196,18 +196,31 @@ struct Lds {
     static constexpr int kByTokens = C * kRow, kByRows = DK * kTok, kSquare = C * kTok;
 };
 
-// 64 rows of a caller's tensor into LDS: as they are (rows), or transposed, or both
-template <class X, int DK, bool ROWS, bool COLS>
-__device__ __forceinline__ void stage_rows(const typename X::E *src, int n, int dk, typename X::E *rows, typename X::E *cols, int tid)
-{
+// 64 rows of a caller's tensor on their way into LDS, as they are, or transposed, or both.  Loads are asked for a chunk ahead (take) and
+// written when the tiles are free (put): with one wavefront per SIMD nothing else hides their latency.
+template <class X, int DK>
+struct RowsStage {
     typedef typename X::E E;
     typedef Lds<X, DK> L;
+    static constexpr int kTasks = 2 * DK;           // four tokens by eight elements each
+    typename X::Exact x[4];
+    __device__ __forceinline__ void take(const E *src, int n, int dk, int tid)
+    {
+        const int tq = tid & 15, o = tid >> 4;
+        if (kTasks < 256 && tid >= kTasks) return;
 #pragma unroll
-    for (int task = tid; task < 2 * DK; task += 256) {
-        const int tq = task & 15, o = task >> 4;            // four tokens, eight elements
-        typename X::Exact x[4];
+        for (int r = 0; r < 4; ++r) x[r] = load8(src + static_cast<int64_t>(min(4 * tq + r, n - 1)) * dk + (8 * o < dk ? 8 * o : 0), true);
+    }
+    template <bool ROWS, bool COLS>
+    __device__ __forceinline__ void put(int n, int dk, E *rows, E *cols, int tid)
+    {
+        const int tq = tid & 15, o = tid >> 4;
+        if (kTasks < 256 && tid >= kTasks) return;
+        if (n < C || dk < DK) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = rows8<X>(src, 4 * tq + r, n, dk, 8 * o);
+            for (int r = 0; r < 4; ++r)
+                x[r] = or_zero(x[r], 4 * tq + r < n && 8 * o < dk);
+        }
         E e[4][8];
 #pragma unroll
         for (int r = 0; r < 4; ++r) __builtin_memcpy(e[r], &x[r], sizeof e[r]);
@@ -229,16 +242,29 @@ __device__ __forceinline__ void stage_rows(const typename X::E *src, int n, int 
             }
         }
     }
-}
+};
 
-// a 64 x 64 fp32 image of the workspace into LDS as an operand in planes
-template <class X, class OPERAND>
-__device__ __forceinline__ void stage_image(const float *src, typename X::E *dst, int tid)
-{
-    constexpr int kTok = C + X::kPad;
+// a 64 x 64 fp32 image of the workspace on its way into LDS as an operand in planes
+struct ImageStage {
+    float x[2][8];
+    __device__ __forceinline__ void take(const float *src, int tid)
+    {
 #pragma unroll
-    for (int task = tid; task < C * C / 8; task += 256) put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, kept<OPERAND>(src + task * 8));
-}
+        for (int i = 0; i < 2; ++i) kept8(src + (tid + 256 * i) * 8, x[i]);
+    }
+    template <class X, class OPERAND>
+    __device__ __forceinline__ void put(typename X::E *dst, int tid) const
+    {
+        constexpr int kTok = C + X::kPad;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int task = tid + 256 * i;
+            OPERAND s;
+            split8(x[i], s);
+            put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, s);
+        }
+    }
+};
 
 // operand from a tile in LDS: rows row0 + lane % 32, 16 k from k0
 template <class X, int STRIDE>
@@ -292,14 +318,29 @@ __device__ __forceinline__ f32x16 exchanged(const OPERAND &first, const OPERAND 
 {
     return mma(first, unit8<X, true>(0, lane), mma(second, unit8<X, true>(1, lane), zero16()));
 }
-// accumulator of 32 rows of a caller's tensor: rows row0 + .., elements k0 .. k0 + 31 in its lanes
+// 64 rows by 32 columns of a caller's tensor on their way into accumulators (rows in registers, columns in lanes)
 template <class X>
-__device__ __forceinline__ f32x16 acc_rows(const typename X::E *p, int row0, int rows, int width, int k0, int lane)
-{
-    const int h = lane >> 5;
-    return mma(rows8<X>(p, row0 + (lane & 31), rows, width, k0 + 8 * h), unit8<X, false>(0, lane),
-               mma(rows8<X>(p, row0 + (lane & 31), rows, width, k0 + 16 + 8 * h), unit8<X, false>(1, lane), zero16()));
-}
+struct ColumnsStage {
+    typename X::Exact x[2][2];
+    __device__ __forceinline__ void take(const typename X::E *p, int n, int width, int k0, int lane)
+    {
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int k = k0 + 16 * b + 8 * (lane >> 5);
+                x[ti][b] = load8(p + static_cast<int64_t>(min(32 * ti + (lane & 31), n - 1)) * width + (k < width ? k : 0), true);
+            }
+    }
+    // (selected without a branch: behind one, the compiler has read the product's accumulators before they were there)
+    __device__ __forceinline__ f32x16 tile(int ti, int n, int width, int k0, int lane) const
+    {
+        typename X::Exact y[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) y[b] = or_zero(x[ti][b], 32 * ti + (lane & 31) < n && k0 + 16 * b + 8 * (lane >> 5) < width);
+        return mma(y[0], unit8<X, false>(0, lane), mma(y[1], unit8<X, false>(1, lane), zero16()));
+    }
+};
 // the way back, rounded to the element type
 template <class X>
 __device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows, int width, int k0, const f32x16 &c, int lane)
@@ -400,22 +441,41 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
     } else if (a.start && active) {
         get_state<DK>(S, a.start + bh * a.start_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
     }
+    RowsStage<X, DK> ks, qs;
+    ImageStage is, ms;
+    ColumnsStage<X> vs;
+    float ds = 0.f;
+    auto take = [&](int c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        const int n = tokens_of(z, z.chunk0 + c);
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        ks.take(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
+        is.take(a.T + at * C * C, tid);
+        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
+        if (active && !trans) vs.take(static_cast<const E *>(a.V) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, n, z.dv, 32 * tile, lane);
+        if (MODE == kOut) {
+            qs.take(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
+            ms.take(a.M + at * C * C, tid);
+        }
+    };
+    if (c0 < c1) take(c0);
     for (int c = c0; c < c1; ++c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         __syncthreads();
-        stage_rows<X, DK, true, true>(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, Ks, Kt, tid);
-        stage_image<X, typename X::Split>(a.T + at * C * C, Ts, tid);
+        ks.template put<true, true>(n, z.dk, Ks, Kt, tid);
+        is.template put<X, typename X::Split>(Ts, tid);
         if (MODE == kOut) {
-            stage_rows<X, DK, true, false>(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, Qs, nullptr, tid);
-            stage_image<X, typename X::Pair>(a.M + at * C * C, Ms, tid);
+            qs.template put<true, false>(n, z.dk, Qs, nullptr, tid);
+            ms.template put<X, typename X::Pair>(Ms, tid);
         }
-        if (tid < 3 * C) dec[tid] = a.dec[at * 3 * C + tid];
+        if (tid < 3 * C) dec[tid] = ds;
+        const ColumnsStage<X> vc = vs;
         __syncthreads();
+        if (c + 1 < c1) take(c + 1);
         if (!active) continue;
         const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
-        const E *V = static_cast<const E *>(a.V) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
         if (MODE == kKeep) {
             float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp;
 #pragma unroll
@@ -436,7 +496,7 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) {
             f32x16 v = zero16();
-            if (MODE != kPre || !trans) v = acc_rows<X>(V, 32 * ti, n, z.dv, 32 * tile, lane);
+            if (MODE != kPre || !trans) v = vc.tile(ti, n, z.dv, 32 * tile, lane);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int i = 32 * ti + acc_row(e, h);
@@ -504,7 +564,9 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
 }
 
 // ------------------------------------------------------------------ states at the segments' starts
-// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T), one wavefront per head and 32 columns.
+// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 32 columns, a
+// wavefront per 32 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and the next step's P
+// and B are in registers before the present one's products begin.
 struct CombineArgs {
     Sizes z;
     const float *carry;             // state to start from (null: zero): carry + bh * carry_head
@@ -517,35 +579,49 @@ struct CombineArgs {
 };
 
 template <class X, int DK, bool REV>
-__global__ __launch_bounds__(64) void delta_combine_kernel(CombineArgs a)
+__global__ __launch_bounds__(2 * DK) void delta_combine_kernel(CombineArgs a)
 {
     typedef typename X::E E;
+    typedef typename X::Split Split;
+    __shared__ Split ops[2][DK / 16][64];
     const Sizes &z = a.z;
-    const int lane = threadIdx.x, h = lane >> 5, col = 32 * blockIdx.x + (lane & 31), bh = blockIdx.y;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5, col = 32 * blockIdx.x + (lane & 31), bh = blockIdx.y;
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
-    f32x16 S[DK / 32];
+    auto segment = [&](int i) { return REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i; };
+    auto rows = [&](const float *state) {
+        const buffer_t b = buffer(state, one);
+        f32x16 s;
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
-    if (a.carry) get_state<DK>(S, a.carry + bh * a.carry_head, z.dk, z.dv, col, h);
+        for (int e = 0; e < 16; ++e) s[e] = get_buffer(b, state_offset(32 * wave + acc_row(e, h), z.dv, col));
+        return s;
+    };
+    Split P[DK / 16];
+    f32x16 B;
+    auto take = [&](int i) {
+        const size_t s = static_cast<size_t>(bh) * z.nseg + segment(i);
+        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + (32 * wave + (lane & 31)) * DK + 8 * h;
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) get8(p + 16 * kb, DK * DK, P[kb]);
+        B = rows(a.add + s * one);
+    };
+    f32x16 S = zero16();
+    if (a.carry) S = rows(a.carry + bh * a.carry_head);
+    if (a.steps > 0) take(0);
     for (int i = 0; i <= a.steps; ++i) {
-        const int s = REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i;
-        put_state<DK>(S, a.at + bh * a.at_head + s * one, z.dk, z.dv, col, h);
+        const buffer_t at = buffer(a.at + bh * a.at_head + segment(i) * one, one);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) put_buffer(at, state_offset(32 * wave + acc_row(e, h), z.dv, col), S[e]);
         if (i == a.steps) break;
-        const E *P = static_cast<const E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + s) * X::kPlanes * DK * DK;
-        f32x16 R[DK / 32];
-        get_state<DK>(R, a.add + (static_cast<size_t>(bh) * z.nseg + s) * one, z.dk, z.dv, col, h);
+        ops[i & 1][2 * wave][lane] = half8<X>(S, 0);
+        ops[i & 1][2 * wave + 1][lane] = half8<X>(S, 1);
+        Split p[DK / 16];
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) {
-            const typename X::Split x = half8<X>(S[kb >> 1], kb & 1);
+        for (int kb = 0; kb < DK / 16; ++kb) p[kb] = P[kb];
+        S = B;
+        __syncthreads();
+        if (i + 1 < a.steps) take(i + 1);
 #pragma unroll
-            for (int t = 0; t < DK / 32; ++t) {
-                typename X::Split p;
-                get8(P + (32 * t + (lane & 31)) * DK + 16 * kb + 8 * h, DK * DK, p);
-                R[t] = mma(p, x, R[t]);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < DK / 32; ++t) S[t] = R[t];
+        for (int kb = 0; kb < DK / 16; ++kb) S = mma(p[kb], ops[i & 1][kb][lane], S);
     }
 }
 
@@ -582,17 +658,35 @@ __global__ __launch_bounds__(256) void delta_rev_kernel(RevArgs a)
 #pragma unroll
     for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
     if (a.end && active) get_state<DK>(S, a.end + bh * a.end_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
+    RowsStage<X, DK> ks, qs;
+    ImageStage is, ms;
+    ColumnsStage<X> os;
+    float ds = 0.f;
+    auto take = [&](int c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        const int n = tokens_of(z, z.chunk0 + c);
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        ks.take(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
+        qs.take(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
+        is.take(a.TT + at * C * C, tid);
+        ms.take(a.MT + at * C * C, tid);
+        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
+        if (active) os.take(static_cast<const E *>(a.dO) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, n, z.dv, 32 * tile, lane);
+    };
+    if (c0 < c1) take(c1 - 1);
     for (int c = c1 - 1; c >= c0; --c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         __syncthreads();
-        stage_rows<X, DK, true, true>(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, Ks, Kt, tid);
-        stage_rows<X, DK, false, true>(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, nullptr, Qt, tid);
-        stage_image<X, typename X::Split>(a.TT + at * C * C, Ts, tid);
-        stage_image<X, typename X::Split>(a.MT + at * C * C, Ms, tid);
-        if (tid < 3 * C) dec[tid] = a.dec[at * 3 * C + tid];
+        ks.template put<true, true>(n, z.dk, Ks, Kt, tid);
+        qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
+        is.template put<X, typename X::Split>(Ts, tid);
+        ms.template put<X, typename X::Split>(Ms, tid);
+        if (tid < 3 * C) dec[tid] = ds;
+        const ColumnsStage<X> oc = os;
         __syncthreads();
+        if (c > c0) take(c - 1);
         if (!active) continue;
         const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
         if (FULL) {
@@ -600,10 +694,9 @@ __global__ __launch_bounds__(256) void delta_rev_kernel(RevArgs a)
 #pragma unroll
             for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
         }
-        const E *dO = static_cast<const E *>(a.dO) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
         f32x16 d[2];
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) d[ti] = acc_rows<X>(dO, 32 * ti, n, z.dv, 32 * tile, lane);
+        for (int ti = 0; ti < 2; ++ti) d[ti] = oc.tile(ti, n, z.dv, 32 * tile, lane);
         // dU = M^T dO + e^{G_C - G} K dS
         f32x16 U[2] = {zero16(), zero16()};
 #pragma unroll
@@ -733,8 +826,13 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
         bs[lane] = lane < n ? strength(a.beta[row0 + lane]) : kBetaFloor;
     }
     qd[tid] = 0.f;
-    stage_rows<X, DK, false, true>(K, n, z.dk, nullptr, Kt, tid);
-    stage_rows<X, DK, false, true>(Q, n, z.dk, nullptr, Qt, tid);
+    {
+        RowsStage<X, DK> ks, qs;
+        ks.take(K, n, z.dk, tid);
+        qs.take(Q, n, z.dk, tid);
+        ks.template put<false, true>(n, z.dk, nullptr, Kt, tid);
+        qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
+    }
     __syncthreads();
 
     // per token: u.dR and v.dV; over the states <S', dS>
@@ -1080,8 +1178,8 @@ struct Passes {
         a.at_head = static_cast<size_t>(p.dk) * p.dv * (rev ? p.nseg : p.nseg + 1);
         a.steps = steps;
         const dim3 grid(p.dvp / 32, p.BH);
-        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 64, 0, st, a);
-        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 64, 0, st, a);
+        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 2 * DK, 0, st, a);
+        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 2 * DK, 0, st, a);
         return hipSuccess;
     }
 
