@@ -43,16 +43,18 @@ constexpr int C = 64;               // tokens per chunk
 constexpr float kBetaFloor = 1e-18f;
 constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 0 either way, and -infinity would make differences NaN
 
-// Element types.  An operand of a 16-deep product is 8 values a lane: lane l holds row (or column) l % 32 and, with h = l / 32,
-// the k of its 8 values: 8 h + 0..7 ("natural") or 8 a + 4 h + r, a = 0, 1, r = 0..3 ("spread": the rows that the lane holds of a
-// 32 x 32 accumulator's 16-row half, so that a product's result is the next product's operand without leaving the registers).
-// Any order will do, as long as both operands have it.
+// Element types.  The passes over the states multiply 16 x 16 tiles, 32 deep: lane l holds row (of a left operand) or column (of a right one)
+// l % 16 and, with q = l / 16, eight of the 32 k: 8 q + 0..7 ("natural") or 16 a + 4 q + r, a = 0, 1, r = 0..3 ("spread": the rows of two
+// accumulators that lie on top of one another, so that a product's result is the next product's operand without leaving the registers).  Any
+// order will do, as long as both operands have it; tiles and images whose rows run over tokens or over columns of the state are stored in spread order.
+// The kernels that are parallel over chunks multiply 32 x 32 tiles, 16 deep, half as many operands to a product: lane l holds row l % 32
+// and the eight places 8 h + 0..7, h = l / 32, of the stored order.
 //
-// bf16: v_mfma_f32_32x32x16_bf16.  The elements of Q, K, V and dO are exact as they are.  Values that are fp32 by their nature enter as
+// bf16: the elements of Q, K, V and dO are exact as they are.  Values that are fp32 by their nature enter as
 // sums of bf16: three (Split: all 24 bits) where fp32 outputs (state, dg, db) hang on them, two (Pair: off by at most 2^-16) where
 // outputs of the element type alone do.  One bf16 (2^-8) would leave the fp32 outputs three digits; with two of them throughout dg was 1.5e-5 off at dk = 16.
 // The matrix instructions of the additional products are not what bounds any of the kernels.
-// fp32: eight v_mfma_f32_32x32x2_f32.
+// fp32: eight fp32 matrix instructions a product, one for each of a lane's k.
 struct Bf {
     typedef uint16_t E;
     typedef bf16x8 Exact;
@@ -78,20 +80,28 @@ __device__ __forceinline__ f32x16 zero16()
     return z;
 }
 
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 // the smallest terms first; terms below 2^-24 of the product are left out
-__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Exact &b, f32x16 c) { return mfma(a, b, c); }
-__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Pair &b, f32x16 c) { return mfma(a, b.hi, mfma(a, b.lo, c)); }
-__device__ __forceinline__ f32x16 mma(const Bf::Pair &a, const Bf::Exact &b, f32x16 c) { return mfma(a.hi, b, mfma(a.lo, b, c)); }
-__device__ __forceinline__ f32x16 mma(const Bf::Pair &a, const Bf::Pair &b, f32x16 c) { return mfma(a.hi, b.hi, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))); }
-__device__ __forceinline__ f32x16 mma(const Bf::Exact &a, const Bf::Split &b, f32x16 c) { return mfma(a, b.hi, mfma(a, b.mid, mfma(a, b.lo, c))); }
-__device__ __forceinline__ f32x16 mma(const Bf::Split &a, const Bf::Exact &b, f32x16 c) { return mfma(a.hi, b, mfma(a.mid, b, mfma(a.lo, b, c))); }
-__device__ __forceinline__ f32x16 mma(const Bf::Split &a, const Bf::Split &b, f32x16 c)
+template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Exact &b, A c) { return mfma(a, b, c); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Pair &b, A c) { return mfma(a, b.hi, mfma(a, b.lo, c)); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Pair &a, const Bf::Exact &b, A c) { return mfma(a.hi, b, mfma(a.lo, b, c)); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Pair &a, const Bf::Pair &b, A c) { return mfma(a.hi, b.hi, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Split &b, A c) { return mfma(a, b.hi, mfma(a, b.mid, mfma(a, b.lo, c))); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Split &a, const Bf::Exact &b, A c) { return mfma(a.hi, b, mfma(a.mid, b, mfma(a.lo, b, c))); }
+template <class A> __device__ __forceinline__ A mma(const Bf::Split &a, const Bf::Split &b, A c)
 {
     return mfma(a.hi, b.hi, mfma(a.hi, b.mid, mfma(a.mid, b.hi, mfma(a.mid, b.mid, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))))));
 }
 __device__ __forceinline__ Bf::Pair lead(const Bf::Split &a) { return Bf::Pair{a.hi, a.mid}; }
 __device__ __forceinline__ const Fp::Exact &lead(const Fp::Exact &a) { return a; }
+__device__ __forceinline__ f32x4 mma(const Fp::Exact &a, const Fp::Exact &b, f32x4 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
 __device__ __forceinline__ f32x16 mma(const Fp::Exact &a, const Fp::Exact &b, f32x16 c)
 {
 #pragma unroll
@@ -99,27 +109,38 @@ __device__ __forceinline__ f32x16 mma(const Fp::Exact &a, const Fp::Exact &b, f3
     return c;
 }
 
-// 8 fp32 values as an operand
+// 8 fp32 values as an operand: pairs, so that two values take one conversion
+__device__ __forceinline__ uint32_t round2(float a, float b)
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+__device__ __forceinline__ float low2(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high2(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ void split8(const float *x, Bf::Split &s)
 {
+    u32x4 hi, mid, lo;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const __bf16 hi = static_cast<__bf16>(x[j]);
-        const float rest = x[j] - static_cast<float>(hi);
-        const __bf16 mid = static_cast<__bf16>(rest);
-        s.hi[j] = hi;
-        s.mid[j] = mid;
-        s.lo[j] = static_cast<__bf16>(rest - static_cast<float>(mid));
+    for (int j = 0; j < 4; ++j) {
+        float a = x[2 * j], b = x[2 * j + 1];
+        hi[j] = round2(a, b);
+        a -= low2(hi[j]);
+        b -= high2(hi[j]);
+        mid[j] = round2(a, b);
+        lo[j] = round2(a - low2(mid[j]), b - high2(mid[j]));
     }
+    s = Bf::Split{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, mid), __builtin_bit_cast(bf16x8, lo)};
 }
 __device__ __forceinline__ void split8(const float *x, Bf::Pair &s)
 {
+    u32x4 hi, lo;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const __bf16 hi = static_cast<__bf16>(x[j]);
-        s.hi[j] = hi;
-        s.lo[j] = static_cast<__bf16>(x[j] - static_cast<float>(hi));
+    for (int j = 0; j < 4; ++j) {
+        hi[j] = round2(x[2 * j], x[2 * j + 1]);
+        lo[j] = round2(x[2 * j] - low2(hi[j]), x[2 * j + 1] - high2(hi[j]));
     }
+    s = Bf::Pair{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
 }
 __device__ __forceinline__ void split8(const float *x, Fp::Exact &s)
 {
@@ -128,8 +149,7 @@ __device__ __forceinline__ void split8(const float *x, Fp::Exact &s)
 }
 __device__ __forceinline__ void round8(const float *x, Bf::Exact &s)
 {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = static_cast<__bf16>(x[j]);
+    s = __builtin_bit_cast(bf16x8, u32x4{round2(x[0], x[1]), round2(x[2], x[3]), round2(x[4], x[5]), round2(x[6], x[7])});
 }
 __device__ __forceinline__ void round8(const float *x, Fp::Exact &s) { split8(x, s); }
 
@@ -153,6 +173,49 @@ __device__ __forceinline__ void get8(const float *p, int, Fp::Exact &x) { x = ge
 __device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Split &x) { put8(p, x.hi); put8(p + plane, x.mid); put8(p + 2 * plane, x.lo); }
 __device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Pair &x) { put8(p, x.hi); put8(p + plane, x.lo); }
 __device__ __forceinline__ void put8(float *p, int, const Fp::Exact &x) { put8(p, x); }
+
+// four fp32 values into planes, and four elements
+__device__ __forceinline__ void put4(uint16_t *p, int plane, const f32x4 &x)
+{
+    u32x2 hi, mid, lo;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float a = x[2 * j], b = x[2 * j + 1];
+        hi[j] = round2(a, b);
+        a -= low2(hi[j]);
+        b -= high2(hi[j]);
+        mid[j] = round2(a, b);
+        lo[j] = round2(a - low2(mid[j]), b - high2(mid[j]));
+    }
+    *reinterpret_cast<u32x2 *>(p) = hi;
+    *reinterpret_cast<u32x2 *>(p + plane) = mid;
+    *reinterpret_cast<u32x2 *>(p + 2 * plane) = lo;
+}
+__device__ __forceinline__ void put4_pair(uint16_t *p, int plane, const f32x4 &x)
+{
+    u32x2 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        hi[j] = round2(x[2 * j], x[2 * j + 1]);
+        lo[j] = round2(x[2 * j] - low2(hi[j]), x[2 * j + 1] - high2(hi[j]));
+    }
+    *reinterpret_cast<u32x2 *>(p) = hi;
+    *reinterpret_cast<u32x2 *>(p + plane) = lo;
+}
+__device__ __forceinline__ void put4(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
+__device__ __forceinline__ void put4_pair(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
+__device__ __forceinline__ void get4(const uint16_t *p, float *x)
+{
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) x[2 * j] = low2(w[j]), x[2 * j + 1] = high2(w[j]);
+}
+__device__ __forceinline__ void get4(const float *p, float *x)
+{
+    const f32x4 w = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = w[j];
+}
 
 // one value
 __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
@@ -194,18 +257,19 @@ __device__ __forceinline__ Fp::Exact load8(const float *p, bool there)
     return x;
 }
 
-// The unit matrix as a right operand, 16 rows from 16 b of a 32 x 32 one.  A product with it turns an operand whose lanes hold rows into
-// an accumulator whose lanes hold columns, exactly (every value times one, plus zeros): rows that lie together in memory become
+// The unit matrix as a right operand, its row 16 b + n in column n (16 columns, natural or spread; 32 columns, spread).  A product with it turns an
+// operand whose lanes hold rows into an accumulator whose lanes hold columns, exactly (every value times one, plus zeros): rows that lie together in memory become
 // accumulators, and accumulators rows that are stored 8 or 16 bytes at a time, without a way through LDS.
-template <class X, bool SPREAD>
+template <class X, int WIDTH, bool SPREAD>
 __device__ __forceinline__ typename X::Exact unit8(int b, int lane)
 {
     float x[8];
     typename X::Exact u;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int k = SPREAD ? 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3) : 8 * (lane >> 5) + j;
-        x[j] = 16 * b + k == (lane & 31) ? 1.f : 0.f;
+        const int part = lane / WIDTH;      // q or h
+        const int k = !SPREAD ? 8 * part + j : WIDTH == 16 ? 16 * (j >> 2) + 4 * part + (j & 3) : 16 * b + 8 * (j >> 2) + 4 * part + (j & 3);
+        x[j] = (WIDTH == 16 ? k - 16 * b : k) == lane % WIDTH ? 1.f : 0.f;
     }
     round8(x, u);
     return u;
@@ -225,30 +289,24 @@ __device__ __forceinline__ void put_buffer(buffer_t b, int offset, float x) { __
 __device__ __forceinline__ void store4(uint16_t *p, const float *x)
 {
     typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any2;
-    uint32_t w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const __bf16 a = static_cast<__bf16>(x[2 * i]), b = static_cast<__bf16>(x[2 * i + 1]);
-        w[i] = __builtin_bit_cast(uint16_t, a) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, b)) << 16;
-    }
-    *reinterpret_cast<u32x2_any2 *>(p) = u32x2_any2{w[0], w[1]};
+    *reinterpret_cast<u32x2_any2 *>(p) = u32x2_any2{round2(x[0], x[1]), round2(x[2], x[3])};
 }
 __device__ __forceinline__ void store4(float *p, const float *x) { *reinterpret_cast<f32x4_any4 *>(p) = f32x4_any4{x[0], x[1], x[2], x[3]}; }
 
-// 8 elements of a caller's row of which a lane takes two runs of four, 8 elements apart (spread order)
+// 8 elements of a caller's row of which a lane takes two runs of four, 16 elements apart (spread order)
 __device__ __forceinline__ Bf::Exact load8_spread(const uint16_t *p, bool first, bool second)
 {
     typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any2;
     u32x2 a = {0, 0}, b = {0, 0};
     if (first) a = *reinterpret_cast<const u32x2_any2 *>(p);
-    if (second) b = *reinterpret_cast<const u32x2_any2 *>(p + 8);
+    if (second) b = *reinterpret_cast<const u32x2_any2 *>(p + 16);
     return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
 }
 __device__ __forceinline__ Fp::Exact load8_spread(const float *p, bool first, bool second)
 {
     f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = {0.f, 0.f, 0.f, 0.f};
     if (first) a = *reinterpret_cast<const f32x4_any4 *>(p);
-    if (second) b = *reinterpret_cast<const f32x4_any4 *>(p + 8);
+    if (second) b = *reinterpret_cast<const f32x4_any4 *>(p + 16);
     return Fp::Exact{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
 
@@ -267,8 +325,8 @@ __device__ __forceinline__ Fp::Exact or_zero(const Fp::Exact &x, bool there)
     return y;
 }
 
-// place of k within a row that is stored in spread order
-__device__ __forceinline__ int spread(int k) { return (k & ~15) | ((k & 4) << 1) | ((k & 8) >> 1) | (k & 3); }
+// place of k within a row that is stored in spread order; of the quad of k that begins at 16 a + 4 q of a group of 32
+__device__ __forceinline__ int spread(int k) { return (k & ~31) | ((k & 12) << 1) | ((k & 16) >> 2) | (k & 3); }
 // row of accumulator register i (32 x 32), within the tile
 __device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 

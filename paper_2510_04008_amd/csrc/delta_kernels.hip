@@ -52,10 +52,11 @@ __device__ __forceinline__ OPERAND kept(const float *p)
     return s;
 }
 
-__device__ __forceinline__ void keep8(float *p, const float *x)
+// a half of a 32 x 32 accumulator (8 rows: k, k + 1, .. and k + 8, ..) into a row of an image
+__device__ __forceinline__ void keep8(float *row, int k, const float *x)
 {
-    reinterpret_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+    *reinterpret_cast<f32x4 *>(row + spread(k)) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4 *>(row + spread(k + 8)) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
 // ------------------------------------------------------------------ what a chunk needs besides the states
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
                 const int i = 32 * ti + (BWD ? row : col), j = 32 * tj + (BWD ? col : row);
                 m[e] = j <= i ? z.scale * expf(static_cast<float>(G[i] - G[j])) * qk[8 * g16 + e] : 0.f;
             }
-            keep8(M + (BWD ? (32 * tj + col) * C + 32 * ti : (32 * ti + col) * C + 32 * tj) + 16 * g16 + 8 * h, m);
+            keep8(M + (BWD ? (32 * tj + col) * C + 32 * ti : (32 * ti + col) * C + 32 * tj), 16 * g16 + 4 * h, m);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -173,17 +174,10 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     __syncthreads();
     if (wave < 2) merge_blocks<32>(A, T, 0, wave, lane);
     __syncthreads();
-    for (int task = tid; task < C * 8; task += 256) {
-        const int row = task >> 3, k0 = 16 * ((task >> 1) & 3), hh = task & 1;
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = T[row][k0 + acc_row(e, hh)];
-        keep8(a.T + at * C * C + row * C + k0 + 8 * hh, x);
-        if (BWD) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = T[k0 + acc_row(e, hh)][row];
-            keep8(a.TT + at * C * C + row * C + k0 + 8 * hh, x);
-        }
+    for (int task = tid; task < C * 16; task += 256) {
+        const int row = task >> 4, k = 4 * (task & 15);
+        *reinterpret_cast<f32x4 *>(a.T + at * C * C + row * C + spread(k)) = *reinterpret_cast<const f32x4 *>(&T[row][k]);
+        if (BWD) *reinterpret_cast<f32x4 *>(a.TT + at * C * C + row * C + spread(k)) = f32x4{T[k][row], T[k + 1][row], T[k + 2][row], T[k + 3][row]};
     }
 }
 
@@ -197,29 +191,25 @@ struct Lds {
 };
 
 // 64 rows of a caller's tensor on their way into LDS, as they are, or transposed, or both.  Loads are asked for a chunk ahead (take) and
-// written when the tiles are free (put): with one wavefront per SIMD nothing else hides their latency.
+// written when the tiles are free (put): with two wavefronts per SIMD nothing else hides their latency.  2 DK tasks of four tokens by eight elements.
 template <class X, int DK>
 struct RowsStage {
     typedef typename X::E E;
     typedef Lds<X, DK> L;
-    static constexpr int kTasks = 2 * DK;           // four tokens by eight elements each
     typename X::Exact x[4];
-    __device__ __forceinline__ void take(const E *src, int n, int dk, int tid)
+    __device__ __forceinline__ void take(const E *src, int n, int dk, int task)
     {
-        const int tq = tid & 15, o = tid >> 4;
-        if (kTasks < 256 && tid >= kTasks) return;
+        const int tq = task & 15, o = task >> 4;
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = load8(src + static_cast<int64_t>(min(4 * tq + r, n - 1)) * dk + (8 * o < dk ? 8 * o : 0), true);
     }
     template <bool ROWS, bool COLS>
-    __device__ __forceinline__ void put(int n, int dk, E *rows, E *cols, int tid)
+    __device__ __forceinline__ void put(int n, int dk, E *rows, E *cols, int task)
     {
-        const int tq = tid & 15, o = tid >> 4;
-        if (kTasks < 256 && tid >= kTasks) return;
+        const int tq = task & 15, o = task >> 4;
         if (n < C || dk < DK) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                x[r] = or_zero(x[r], 4 * tq + r < n && 8 * o < dk);
+            for (int r = 0; r < 4; ++r) x[r] = or_zero(x[r], 4 * tq + r < n && 8 * o < dk);
         }
         E e[4][8];
 #pragma unroll
@@ -228,37 +218,39 @@ struct RowsStage {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    E *to = rows + (4 * tq + r) * L::kRow + 16 * (o >> 1) + 8 * q + 4 * (o & 1);
-                    __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), &e[r][4 * q], 4 * sizeof(E));
+                for (int i = 0; i < 2; ++i) {
+                    E *to = rows + (4 * tq + r) * L::kRow + spread(8 * o + 4 * i);
+                    __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), &e[r][4 * i], 4 * sizeof(E));
                 }
         }
         if (COLS) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 E v[4] = {e[0][k], e[1][k], e[2][k], e[3][k]};
-                E *to = cols + (8 * o + k) * L::kTok + 16 * (tq >> 2) + 8 * (tq & 1) + 4 * ((tq >> 1) & 1);
+                E *to = cols + (8 * o + k) * L::kTok + spread(4 * tq);
                 __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), v, 4 * sizeof(E));
             }
         }
     }
 };
 
-// a 64 x 64 fp32 image of the workspace on its way into LDS as an operand in planes
+// a 64 x 64 fp32 image of the workspace on its way into LDS as an operand in planes, by 512 threads or 256
+template <int THREADS>
 struct ImageStage {
-    float x[2][8];
+    static constexpr int kEach = 512 / THREADS;
+    float x[kEach][8];
     __device__ __forceinline__ void take(const float *src, int tid)
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) kept8(src + (tid + 256 * i) * 8, x[i]);
+        for (int i = 0; i < kEach; ++i) kept8(src + (tid + THREADS * i) * 8, x[i]);
     }
     template <class X, class OPERAND>
     __device__ __forceinline__ void put(typename X::E *dst, int tid) const
     {
         constexpr int kTok = C + X::kPad;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int task = tid + 256 * i;
+        for (int i = 0; i < kEach; ++i) {
+            const int task = tid + THREADS * i;
             OPERAND s;
             split8(x[i], s);
             put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, s);
@@ -266,135 +258,106 @@ struct ImageStage {
     }
 };
 
-// operand from a tile in LDS: rows row0 + lane % 32, 16 k from k0
+// left operand from a tile in LDS: rows row0 + lane % 16, 32 places from k0
 template <class X, int STRIDE>
 __device__ __forceinline__ typename X::Exact tile8(const typename X::E *t, int row0, int k0, int lane)
 {
-    return get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5));
+    return get8(t + (row0 + (lane & 15)) * STRIDE + k0 + 8 * (lane >> 4));
 }
 template <class OPERAND, int STRIDE, class E>
 __device__ __forceinline__ OPERAND tile8s(const E *t, int row0, int k0, int lane)
 {
     OPERAND x;
-    get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5), C * STRIDE, x);
+    get8(t + (row0 + (lane & 15)) * STRIDE + k0 + 8 * (lane >> 4), C * STRIDE, x);
     return x;
 }
 
-// 8 rows (one half of an accumulator) times a factor per row, as an operand
-template <class X>
-__device__ __forceinline__ typename X::Split scaled8(const f32x16 &c, int half16, const float *factor, int h)
-{
-    float x[8];
-    typename X::Split s;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e] * factor[acc_row(8 * half16 + e, h)];
-    split8(x, s);
-    return s;
-}
-template <class X>
-__device__ __forceinline__ typename X::Split half8(const f32x16 &c, int half16)
-{
-    float x[8];
-    typename X::Split s;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e];
-    split8(x, s);
-    return s;
-}
+// The compiler would ask for the operands of later products long before it has registers for them.
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
-template <class X>
-__device__ __forceinline__ typename X::Exact round8_of(const f32x16 &c, int half16)
+// two accumulators on top of one another as a right operand
+template <class OPERAND>
+__device__ __forceinline__ OPERAND operand(const f32x4 &first, const f32x4 &second)
 {
-    float x[8];
+    const float x[8] = {first[0], first[1], first[2], first[3], second[0], second[1], second[2], second[3]};
+    OPERAND s;
+    split8(x, s);
+    return s;
+}
+template <class X>
+__device__ __forceinline__ typename X::Exact rounded(const f32x4 &first, const f32x4 &second)
+{
+    const float x[8] = {first[0], first[1], first[2], first[3], second[0], second[1], second[2], second[3]};
     typename X::Exact s;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = c[8 * half16 + e];
     round8(x, s);
     return s;
 }
-// 32 x 32 accumulator with rows and columns exchanged
-template <class X, class OPERAND>
-__device__ __forceinline__ f32x16 exchanged(const OPERAND &first, const OPERAND &second, int lane)
-{
-    return mma(first, unit8<X, true>(0, lane), mma(second, unit8<X, true>(1, lane), zero16()));
-}
-// 64 rows by 32 columns of a caller's tensor on their way into accumulators (rows in registers, columns in lanes)
+
+// 64 rows by 16 columns of a caller's tensor on their way into accumulators (rows in registers, columns in lanes)
 template <class X>
 struct ColumnsStage {
-    typename X::Exact x[2][2];
+    typename X::Exact x[4];
     __device__ __forceinline__ void take(const typename X::E *p, int n, int width, int k0, int lane)
     {
+        const int k = k0 + 8 * ((lane >> 4) & 1);
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int k = k0 + 16 * b + 8 * (lane >> 5);
-                x[ti][b] = load8(p + static_cast<int64_t>(min(32 * ti + (lane & 31), n - 1)) * width + (k < width ? k : 0), true);
-            }
+        for (int ti = 0; ti < 4; ++ti) x[ti] = load8(p + static_cast<int64_t>(min(16 * ti + (lane & 15), n - 1)) * width + (k < width ? k : 0), true);
     }
     // (selected without a branch: behind one, the compiler has read the product's accumulators before they were there)
-    __device__ __forceinline__ f32x16 tile(int ti, int n, int width, int k0, int lane) const
+    __device__ __forceinline__ f32x4 tile(int ti, int n, int width, int k0, int lane) const
     {
-        typename X::Exact y[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) y[b] = or_zero(x[ti][b], 32 * ti + (lane & 31) < n && k0 + 16 * b + 8 * (lane >> 5) < width);
-        return mma(y[0], unit8<X, false>(0, lane), mma(y[1], unit8<X, false>(1, lane), zero16()));
+        const bool there = lane < 32 && 16 * ti + (lane & 15) < n && k0 + 8 * ((lane >> 4) & 1) < width;
+        return mma(or_zero(x[ti], there), unit8<X, 16, false>(0, lane), zero4());
     }
 };
-// the way back, rounded to the element type
+// the way back, rounded to the element type: two accumulators on top of one another, 32 rows from row0
 template <class X>
-__device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows, int width, int k0, const f32x16 &c, int lane)
+__device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows, int width, int k0, const f32x4 &first, const f32x4 &second, int lane)
 {
-    const f32x16 t = exchanged<X>(round8_of<X>(c, 0), round8_of<X>(c, 1), lane);
-    const int row = row0 + (lane & 31);
+    const typename X::Exact x = rounded<X>(first, second);
+    const int k = k0 + 4 * (lane >> 4);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int k = k0 + 8 * q + 4 * (lane >> 5);
-        const float x[4] = {t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
-        if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, x);
+    for (int b = 0; b < 2; ++b) {
+        const f32x4 t = mma(x, unit8<X, 16, true>(b, lane), zero4());
+        const int row = row0 + 16 * b + (lane & 15);
+        const float y[4] = {t[0], t[1], t[2], t[3]};
+        if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, y);
     }
 }
-// rows of an image in the workspace, fp32 or in planes: row of the accumulator -> row of the image, its 32 columns in spread order from k0
+// two accumulators on top of one another into an image of the workspace, 32 rows from row0, columns k0 .. k0 + 15 in spread order
 template <class X>
-__device__ __forceinline__ void keep_rows(float *p, int row0, int width, int k0, const f32x16 &c, int lane)
+__device__ __forceinline__ void keep_rows(float *p, int row0, int width, int k0, const f32x4 &first, const f32x4 &second, int lane)
 {
-    const f32x16 t = exchanged<X>(half8<X>(c, 0), half8<X>(c, 1), lane);
-    float *to = p + (row0 + (lane & 31)) * width + k0 + 8 * (lane >> 5);
+    const typename X::Split x = operand<typename X::Split>(first, second);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(to + 16 * (q >> 1) + 4 * (q & 1)) = f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
-}
-template <class X>
-__device__ __forceinline__ void keep_planes(typename X::E *p, int plane, int row0, int width, int k0, const f32x16 &c, int lane)
-{
-    const f32x16 t = exchanged<X>(half8<X>(c, 0), half8<X>(c, 1), lane);
-#pragma unroll
-    for (int g16 = 0; g16 < 2; ++g16) put8(p + (row0 + (lane & 31)) * width + k0 + 16 * g16 + 8 * (lane >> 5), plane, half8<X>(t, g16));
+    for (int b = 0; b < 2; ++b)
+        *reinterpret_cast<f32x4 *>(p + (row0 + 16 * b + (lane & 15)) * width + spread(k0 + 4 * (lane >> 4))) = mma(x, unit8<X, 16, true>(b, lane), zero4());
 }
 
-// accumulator of 32 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written
+// a wavefront's 16 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written
 __device__ __forceinline__ int state_offset(int row, int dv, int col) { return col < dv ? 4 * (row * dv + col) : kNowhere; }
-template <int DK>
-__device__ __forceinline__ void get_state(f32x16 (&S)[DK / 32], const float *state, int dk, int dv, int col, int h)
+template <int TILES>
+__device__ __forceinline__ void get_state(f32x4 (&S)[TILES], const float *state, int dk, int dv, int row0, int col, int lane)
 {
     const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t)
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) S[t][e] = get_buffer(b, state_offset(32 * t + acc_row(e, h), dv, col));
+        for (int e = 0; e < 4; ++e) S[t][e] = get_buffer(b, state_offset(row0 + 16 * t + 4 * (lane >> 4) + e, dv, col));
 }
-template <int DK>
-__device__ __forceinline__ void put_state(const f32x16 (&S)[DK / 32], float *state, int dk, int dv, int col, int h)
+template <int TILES>
+__device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state, int dk, int dv, int row0, int col, int lane)
 {
     const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t)
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) put_buffer(b, state_offset(32 * t + acc_row(e, h), dv, col), S[t][e]);
+        for (int e = 0; e < 4; ++e) put_buffer(b, state_offset(row0 + 16 * t + 4 * (lane >> 4) + e, dv, col), S[t][e]);
 }
 
 // ------------------------------------------------------------------ the states, chunk after chunk
-// One workgroup per segment, head and four tiles of 32 columns of the state; a wavefront keeps its columns of the state in
-// accumulators from chunk to chunk (DK x 32 fp32), where they are at once the right operand of the products with K and Q.
+// One workgroup per segment, head and up to eight (four) tiles of 16 columns of the state; a wavefront keeps its columns of the state in
+// accumulators from chunk to chunk (DK x 16 fp32), where they are at once the right operand of the products with K and Q.
 // Columns never meet, so wavefronts share the tiles in LDS and nothing else.
 enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's transition and state from zero; states and U for the backward pass
 
@@ -412,66 +375,77 @@ struct ScanArgs {
     float *S, *U;                   // kKeep: states at the chunks' starts and behind the last, and U, rows in spread order
 };
 
-template <class X, int DK, int MODE>
-__global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
+template <class X, int DK, int THREADS, int MODE>
+__global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 {
     typedef typename X::E E;
+    typedef typename X::Split Split;
     typedef Lds<X, DK> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPlanes * L::kSquare;
     E *Ms = Qs + L::kByTokens;
     float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPairPlanes * L::kSquare : Qs);
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4, col = lane & 15;
     const int bh = blockIdx.z, seg = blockIdx.y;
-    const int vtiles = z.dvp / 32, tile = blockIdx.x * 4 + wave;
+    const int vtiles = z.dvp / 16, tile = blockIdx.x * (THREADS / 64) + wave;
     const bool trans = MODE == kPre && tile >= vtiles;
-    const bool active = MODE == kPre ? tile < vtiles + (a.transitions ? DK / 32 : 0) : tile < vtiles;
-    const int vcol = 32 * tile + col;                   // column of V (or, less the tiles of V, of the transition)
+    const bool active = MODE == kPre ? tile < vtiles + (a.transitions ? DK / 16 : 0) : tile < vtiles;
+    const int vcol = 16 * tile + col;                   // column of V (or, less the tiles of V, of the transition)
     const int c0 = (z.seg0 + seg) * z.seg_chunks - z.chunk0, c1 = min(c0 + z.seg_chunks, z.chunks);
+    static_assert(THREADS >= 4 * DK, "a thread stages rows of K or of Q");
+    const bool has_k = tid < 2 * DK, has_q = MODE == kOut && tid >= 2 * DK && tid < 4 * DK;
+    const int task = has_k ? tid : tid - 2 * DK;
 
-    f32x16 S[DK / 32];
+    f32x4 S[DK / 16];
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
+    for (int t = 0; t < DK / 16; ++t) S[t] = zero4();
     if (trans) {
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t)
+        for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[t][e] = 32 * t + acc_row(e, h) == vcol - z.dvp ? 1.f : 0.f;
+            for (int e = 0; e < 4; ++e) S[t][e] = 16 * t + 4 * q + e == vcol - z.dvp ? 1.f : 0.f;
     } else if (a.start && active) {
-        get_state<DK>(S, a.start + bh * a.start_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
+        get_state(S, a.start + bh * a.start_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, 0, vcol, lane);
     }
-    RowsStage<X, DK> ks, qs;
-    ImageStage is, ms;
+    constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
+    RowsStage<X, DK> rows;
+    ImageStage<THREADS> is, ms;
     ColumnsStage<X> vs;
     float ds = 0.f;
     auto take = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
-        ks.take(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
-        is.take(a.T + at * C * C, tid);
-        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
-        if (active && !trans) vs.take(static_cast<const E *>(a.V) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, n, z.dv, 32 * tile, lane);
-        if (MODE == kOut) {
-            qs.take(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
-            ms.take(a.M + at * C * C, tid);
+        if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
+        if (kAhead) {
+            is.take(a.T + at * C * C, tid);
+            if (MODE == kOut) ms.take(a.M + at * C * C, tid);
         }
+        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
     };
-    if (c0 < c1) take(c0);
+    auto take_columns = [&](int c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        if (!trans) vs.take(static_cast<const E *>(a.V) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, tokens_of(z, z.chunk0 + c), z.dv, 16 * tile, lane);
+    };
+    if (c0 < c1) {
+        take(c0);
+        if (active) take_columns(c0);
+    }
     for (int c = c0; c < c1; ++c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         __syncthreads();
-        ks.template put<true, true>(n, z.dk, Ks, Kt, tid);
-        is.template put<X, typename X::Split>(Ts, tid);
+        if (has_k) rows.template put<true, true>(n, z.dk, Ks, Kt, task);
+        if (has_q) rows.template put<true, false>(n, z.dk, Qs, nullptr, task);
+        if (!kAhead) is.take(a.T + at * C * C, tid);
+        is.template put<X, Split>(Ts, tid);
         if (MODE == kOut) {
-            qs.template put<true, false>(n, z.dk, Qs, nullptr, tid);
+            if (!kAhead) ms.take(a.M + at * C * C, tid);
             ms.template put<X, typename X::Pair>(Ms, tid);
         }
         if (tid < 3 * C) dec[tid] = ds;
-        const ColumnsStage<X> vc = vs;
         __syncthreads();
         if (c + 1 < c1) take(c + 1);
         if (!active) continue;
@@ -479,93 +453,108 @@ __global__ __launch_bounds__(256) void delta_scan_kernel(ScanArgs a)
         if (MODE == kKeep) {
             float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp;
 #pragma unroll
-            for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+            for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
         }
+        fence();
         // K S, and Q S for the outputs
-        f32x16 R[2] = {zero16(), zero16()}, O[2] = {zero16(), zero16()};
+        f32x4 R[4], O[4];
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) {
-            const typename X::Split s = half8<X>(S[kb >> 1], kb & 1);
+        for (int ti = 0; ti < 4; ++ti) R[ti] = O[ti] = zero4();
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti) {
-                R[ti] = mma(tile8<X, L::kRow>(Ks, 32 * ti, 16 * kb, lane), s, R[ti]);
-                if (MODE == kOut) O[ti] = mma(tile8<X, L::kRow>(Qs, 32 * ti, 16 * kb, lane), lead(s), O[ti]);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
+            if (sizeof(E) == 4) fence();
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti) {
+                R[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, R[ti]);
+                if (MODE == kOut) O[ti] = mma(tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), lead(s), O[ti]);
             }
         }
+        fence();
         // b (V - e^G K S)
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) {
-            f32x16 v = zero16();
-            if (MODE != kPre || !trans) v = vc.tile(ti, n, z.dv, 32 * tile, lane);
+        for (int ti = 0; ti < 4; ++ti) {
+            f32x4 v = zero4();
+            if (MODE != kPre || !trans) v = vs.tile(ti, n, z.dv, 16 * tile, lane);
+            const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + 16 * ti + 4 * q), b = *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = 32 * ti + acc_row(e, h);
-                R[ti][e] = beta[i] * (v[e] - eG[i] * R[ti][e]);
-                if (MODE == kOut) O[ti][e] *= z.scale * eG[i];
+            for (int e = 0; e < 4; ++e) {
+                R[ti][e] = b[e] * (v[e] - g[e] * R[ti][e]);
+                if (MODE == kOut) O[ti][e] *= z.scale * g[e];
             }
         }
+        if (c + 1 < c1) take_columns(c + 1);
+        fence();
         // U = T R, and the outputs' M U
-        f32x16 U[2] = {zero16(), zero16()};
+        f32x4 U[4];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const typename X::Split r = half8<X>(R[kb >> 1], kb & 1);
+        for (int ti = 0; ti < 4; ++ti) U[ti] = zero4();
 #pragma unroll
-            for (int ti = kb >> 1; ti < 2; ++ti) U[ti] = mma(tile8s<typename X::Split, L::kTok>(Ts, 32 * ti, 16 * kb, lane), r, U[ti]);
+        for (int kb = 0; kb < 2; ++kb) {
+            const Split r = operand<Split>(R[2 * kb], R[2 * kb + 1]);
+            if (sizeof(E) == 4) fence();
+#pragma unroll
+            for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
         }
         if (MODE == kOut) {
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                const typename X::Split u = half8<X>(U[kb >> 1], kb & 1);
-#pragma unroll
-                for (int ti = kb >> 1; ti < 2; ++ti) O[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ms, 32 * ti, 16 * kb, lane), lead(u), O[ti]);
-            }
             E *out = static_cast<E *>(a.O) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti) store_rows<X>(out, 32 * ti, n, z.dv, 32 * tile, O[ti], lane);
+            for (int kb = 0; kb < 2; ++kb) {
+                const typename X::Pair u = operand<typename X::Pair>(U[2 * kb], U[2 * kb + 1]);
+#pragma unroll
+                for (int ti = 2 * kb; ti < 4; ++ti) O[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ms, 16 * ti, 32 * kb, lane), u, O[ti]);
+                store_rows<X>(out, 32 * kb, n, z.dv, 16 * tile, O[2 * kb], O[2 * kb + 1], lane);
+            }
         }
         if (MODE == kKeep) {
             float *keep = a.U + at * C * z.dvp;
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti) keep_rows<X>(keep, 32 * ti, z.dvp, 32 * tile, U[ti], lane);
+            for (int ti = 0; ti < 4; ti += 2) keep_rows<X>(keep, 16 * ti, z.dvp, 16 * tile, U[ti], U[ti + 1], lane);
         }
+        fence();
         // the state behind the chunk
         const float whole = eG[C - 1];
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t)
+        for (int t = 0; t < DK / 16; ++t) S[t] *= whole;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[t][e] *= whole;
+        for (int kb = 0; kb < 2; ++kb) {
+            const f32x4 e0 = *reinterpret_cast<const f32x4 *>(eEnd + 32 * kb + 4 * q), e1 = *reinterpret_cast<const f32x4 *>(eEnd + 32 * kb + 16 + 4 * q);
+            const Split u = operand<Split>(U[2 * kb] * e0, U[2 * kb + 1] * e1);
+            if (sizeof(E) == 4) fence();
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const typename X::Split u = scaled8<X>(U[kb >> 1], kb & 1, eEnd + 32 * (kb >> 1), h);
-#pragma unroll
-            for (int t = 0; t < DK / 32; ++t) S[t] = mma(tile8<X, L::kTok>(Kt, 32 * t, 16 * kb, lane), u, S[t]);
+            for (int t = 0; t < DK / 16; ++t) S[t] = mma(tile8<X, L::kTok>(Kt, 16 * t, 32 * kb, lane), u, S[t]);
         }
     }
     if (!active) return;
     if (MODE == kKeep && c1 == z.chunks) {
         float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+        for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
     }
     if (trans) {
+        // P as a left operand: rows of the accumulators, its columns spread; P^T: the columns, whose rows are a lane's eight values
         E *P = static_cast<E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
         E *PT = static_cast<E *>(a.PT) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
-        const int k = vcol - z.dvp;
+        const int k0 = 16 * tile - z.dvp;
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t) {
-            keep_planes<X>(P, DK * DK, 32 * t, DK, 32 * tile - z.dvp, S[t], lane);
+        for (int t = 0; t < DK / 16; t += 2) {
+            const Split x = operand<Split>(S[t], S[t + 1]);
+            put8(PT + (k0 + col) * DK + 16 * t + 8 * q, DK * DK, x);
 #pragma unroll
-            for (int g16 = 0; g16 < 2; ++g16) put8(PT + k * DK + 32 * t + 16 * g16 + 8 * h, DK * DK, half8<X>(S[t], g16));
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 y = mma(x, unit8<X, 16, true>(b, lane), zero4());
+                put4(P + (16 * t + 16 * b + col) * DK + spread(k0 + 4 * q), DK * DK, y);
+            }
         }
         return;
     }
     if (a.final_state && (MODE == kPre || seg == z.segs - 1))
-        put_state<DK>(S, a.final_state + bh * a.final_head + (MODE == kPre ? static_cast<size_t>(seg) * z.dk * z.dv : 0), z.dk, z.dv, vcol, h);
+        put_state(S, a.final_state + bh * a.final_head + (MODE == kPre ? static_cast<size_t>(seg) * z.dk * z.dv : 0), z.dk, z.dv, 0, vcol, lane);
 }
 
 // ------------------------------------------------------------------ states at the segments' starts
-// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 32 columns, a
-// wavefront per 32 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and the next step's P
+// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 columns, a
+// wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and the next step's P
 // and B are in registers before the present one's products begin.
 struct CombineArgs {
     Sizes z;
@@ -579,49 +568,46 @@ struct CombineArgs {
 };
 
 template <class X, int DK, bool REV>
-__global__ __launch_bounds__(2 * DK) void delta_combine_kernel(CombineArgs a)
+__global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 {
     typedef typename X::E E;
     typedef typename X::Split Split;
-    __shared__ Split ops[2][DK / 16][64];
+    __shared__ __attribute__((aligned(16))) E ops[2][X::kPlanes][DK / 32][64 * 8];
     const Sizes &z = a.z;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5, col = 32 * blockIdx.x + (lane & 31), bh = blockIdx.y;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane >> 4, col = 16 * blockIdx.x + (lane & 15), bh = blockIdx.y;
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
     auto segment = [&](int i) { return REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i; };
-    auto rows = [&](const float *state) {
-        const buffer_t b = buffer(state, one);
-        f32x16 s;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = get_buffer(b, state_offset(32 * wave + acc_row(e, h), z.dv, col));
-        return s;
-    };
-    Split P[DK / 16];
-    f32x16 B;
+    Split P[DK / 32];
+    f32x4 B[1], S[1] = {zero4()};
     auto take = [&](int i) {
         const size_t s = static_cast<size_t>(bh) * z.nseg + segment(i);
-        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + (32 * wave + (lane & 31)) * DK + 8 * h;
+        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + (16 * wave + (lane & 15)) * DK + 8 * q;
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) get8(p + 16 * kb, DK * DK, P[kb]);
-        B = rows(a.add + s * one);
+        for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, P[kb]);
+        get_state(B, a.add + s * one, z.dk, z.dv, 16 * wave, col, lane);
     };
-    f32x16 S = zero16();
-    if (a.carry) S = rows(a.carry + bh * a.carry_head);
+    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, 16 * wave, col, lane);
     if (a.steps > 0) take(0);
     for (int i = 0; i <= a.steps; ++i) {
-        const buffer_t at = buffer(a.at + bh * a.at_head + segment(i) * one, one);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) put_buffer(at, state_offset(32 * wave + acc_row(e, h), z.dv, col), S[e]);
+        put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, 16 * wave, col, lane);
         if (i == a.steps) break;
-        ops[i & 1][2 * wave][lane] = half8<X>(S, 0);
-        ops[i & 1][2 * wave + 1][lane] = half8<X>(S, 1);
-        Split p[DK / 16];
+        // the lane's four rows are half of its eight places in the operand of 32 rows
+        put4(&ops[i & 1][0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[0]);
+        Split p[DK / 32];
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) p[kb] = P[kb];
-        S = B;
+        for (int kb = 0; kb < DK / 32; ++kb) p[kb] = P[kb];
+        S[0] = B[0];
+        f32x4 more = zero4();
         __syncthreads();
         if (i + 1 < a.steps) take(i + 1);
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) S = mma(p[kb], ops[i & 1][kb][lane], S);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            Split s;
+            get8(&ops[i & 1][0][kb][lane * 8], DK / 32 * 64 * 8, s);
+            if (kb & 1) more = mma(p[kb], s, more);
+            else S[0] = mma(p[kb], s, S[0]);
+        }
+        S[0] += more;
     }
 }
 
@@ -639,52 +625,65 @@ struct RevArgs {
     float *dS, *dR;                 // FULL: cotangents at the chunks' ends, and dR, rows in spread order
 };
 
-template <class X, int DK, bool FULL>
-__global__ __launch_bounds__(256) void delta_rev_kernel(RevArgs a)
+template <class X, int DK, int THREADS, bool FULL>
+__global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 {
     typedef typename X::E E;
+    typedef typename X::Split Split;
     typedef Lds<X, DK> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Qt = Kt + L::kByRows, *Ts = Qt + L::kByRows, *Ms = Ts + X::kPlanes * L::kSquare;
     float *dec = reinterpret_cast<float *>(Ms + X::kPlanes * L::kSquare);
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4;
     const int bh = blockIdx.z, seg = blockIdx.y + a.seg_skip;
-    const int tile = blockIdx.x * 4 + wave, vcol = 32 * tile + (lane & 31);
-    const bool active = tile < z.dvp / 32;
+    const int tile = blockIdx.x * (THREADS / 64) + wave, vcol = 16 * tile + (lane & 15);
+    const bool active = tile < z.dvp / 16;
     const int c0 = (z.seg0 + seg) * z.seg_chunks - z.chunk0, c1 = min(c0 + z.seg_chunks, z.chunks);
+    static_assert(THREADS >= 4 * DK, "a thread stages rows of K or of Q");
+    const bool has_k = tid < 2 * DK, has_q = tid >= 2 * DK && tid < 4 * DK;
+    const int task = has_k ? tid : tid - 2 * DK;
 
-    f32x16 S[DK / 32];
+    f32x4 S[DK / 16];
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t) S[t] = zero16();
-    if (a.end && active) get_state<DK>(S, a.end + bh * a.end_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, vcol, h);
-    RowsStage<X, DK> ks, qs;
-    ImageStage is, ms;
+    for (int t = 0; t < DK / 16; ++t) S[t] = zero4();
+    if (a.end && active) get_state(S, a.end + bh * a.end_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, 0, vcol, lane);
+    constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
+    RowsStage<X, DK> rows;
+    ImageStage<THREADS> is, ms;
     ColumnsStage<X> os;
     float ds = 0.f;
     auto take = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
-        ks.take(static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
-        qs.take(static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, tid);
-        is.take(a.TT + at * C * C, tid);
-        ms.take(a.MT + at * C * C, tid);
+        if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
+        if (kAhead) {
+            is.take(a.TT + at * C * C, tid);
+            ms.take(a.MT + at * C * C, tid);
+        }
         if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
-        if (active) os.take(static_cast<const E *>(a.dO) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, n, z.dv, 32 * tile, lane);
     };
-    if (c0 < c1) take(c1 - 1);
+    auto take_columns = [&](int c) {
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
+        os.take(static_cast<const E *>(a.dO) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv, tokens_of(z, z.chunk0 + c), z.dv, 16 * tile, lane);
+    };
+    if (c0 < c1) {
+        take(c1 - 1);
+        if (active) take_columns(c1 - 1);
+    }
     for (int c = c1 - 1; c >= c0; --c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         __syncthreads();
-        ks.template put<true, true>(n, z.dk, Ks, Kt, tid);
-        qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
-        is.template put<X, typename X::Split>(Ts, tid);
-        ms.template put<X, typename X::Split>(Ms, tid);
+        if (has_k) rows.template put<true, true>(n, z.dk, Ks, Kt, task);
+        if (has_q) rows.template put<false, true>(n, z.dk, nullptr, Qt, task);
+        if (!kAhead) is.take(a.TT + at * C * C, tid);
+        is.template put<X, Split>(Ts, tid);
+        if (!kAhead) ms.take(a.MT + at * C * C, tid);
+        ms.template put<X, Split>(Ms, tid);
         if (tid < 3 * C) dec[tid] = ds;
-        const ColumnsStage<X> oc = os;
         __syncthreads();
         if (c > c0) take(c - 1);
         if (!active) continue;
@@ -692,76 +691,79 @@ __global__ __launch_bounds__(256) void delta_rev_kernel(RevArgs a)
         if (FULL) {
             float *keep = a.dS + at * DK * z.dvp;
 #pragma unroll
-            for (int t = 0; t < DK / 32; ++t) keep_rows<X>(keep, 32 * t, z.dvp, 32 * tile, S[t], lane);
+            for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
         }
-        f32x16 d[2];
+        f32x4 d[4];
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) d[ti] = oc.tile(ti, n, z.dv, 32 * tile, lane);
+        for (int ti = 0; ti < 4; ++ti) d[ti] = os.tile(ti, n, z.dv, 16 * tile, lane);
+        if (kAhead && c > c0) take_columns(c - 1);
+        fence();
         // dU = M^T dO + e^{G_C - G} K dS
-        f32x16 U[2] = {zero16(), zero16()};
+        f32x4 U[4];
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) {
-            const typename X::Split s = half8<X>(S[kb >> 1], kb & 1);
+        for (int ti = 0; ti < 4; ++ti) U[ti] = zero4();
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti) U[ti] = mma(tile8<X, L::kRow>(Ks, 32 * ti, 16 * kb, lane), s, U[ti]);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
+            if (sizeof(E) == 4) fence();
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti) U[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, U[ti]);
         }
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti)
+        for (int ti = 0; ti < 4; ++ti) U[ti] *= *reinterpret_cast<const f32x4 *>(eEnd + 16 * ti + 4 * q);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) U[ti][e] *= eEnd[32 * ti + acc_row(e, h)];
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename X::Exact o = rounded<X>(d[2 * kb], d[2 * kb + 1]);      // (exact: elements of dO)
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const typename X::Exact o = round8_of<X>(d[kb >> 1], kb & 1);      // (exact: elements of dO)
-#pragma unroll
-            for (int ti = 0; ti <= kb >> 1; ++ti) U[ti] = mma(tile8s<typename X::Split, L::kTok>(Ms, 32 * ti, 16 * kb, lane), o, U[ti]);
+            for (int ti = 0; ti < 2 * kb + 2; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ms, 16 * ti, 32 * kb, lane), o, U[ti]);
         }
+        fence();
         // dR = T^T dU
-        f32x16 R[2] = {zero16(), zero16()};
+        f32x4 R[4];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const typename X::Split u = half8<X>(U[kb >> 1], kb & 1);
+        for (int ti = 0; ti < 4; ++ti) R[ti] = zero4();
 #pragma unroll
-            for (int ti = 0; ti <= kb >> 1; ++ti) R[ti] = mma(tile8s<typename X::Split, L::kTok>(Ts, 32 * ti, 16 * kb, lane), u, R[ti]);
+        for (int kb = 0; kb < 2; ++kb) {
+            const Split u = operand<Split>(U[2 * kb], U[2 * kb + 1]);
+            if (sizeof(E) == 4) fence();
+#pragma unroll
+            for (int ti = 0; ti < 2 * kb + 2; ++ti) R[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), u, R[ti]);
         }
+        f32x4 b[4];
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti) b[ti] = *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q);
         if (FULL) {
             float *keep = a.dR + at * C * z.dvp;
             E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti) {
-                keep_rows<X>(keep, 32 * ti, z.dvp, 32 * tile, R[ti], lane);
-                f32x16 v;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = beta[32 * ti + acc_row(e, h)] * R[ti][e];
-                store_rows<X>(dV, 32 * ti, n, z.dv, 32 * tile, v, lane);
+            for (int ti = 0; ti < 4; ti += 2) {
+                keep_rows<X>(keep, 16 * ti, z.dvp, 16 * tile, R[ti], R[ti + 1], lane);
+                store_rows<X>(dV, 16 * ti, n, z.dv, 16 * tile, b[ti] * R[ti], b[ti + 1] * R[ti + 1], lane);
             }
         }
+        fence();
         // the cotangent before the chunk
         const float whole = eG[C - 1];
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t)
+        for (int t = 0; t < DK / 16; ++t) S[t] *= whole;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[t][e] *= whole;
+        for (int kb = 0; kb < 2; ++kb) {
+            f32x4 g[2];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            float x[8], y[8];
-            typename X::Split o, r;
+            for (int i = 0; i < 2; ++i) g[i] = *reinterpret_cast<const f32x4 *>(eG + 32 * kb + 16 * i + 4 * q);
+            const Split o = operand<Split>(d[2 * kb] * (z.scale * g[0]), d[2 * kb + 1] * (z.scale * g[1]));
+            if (sizeof(E) == 4) fence();
+            const Split r = operand<Split>(R[2 * kb] * (-b[2 * kb] * g[0]), R[2 * kb + 1] * (-b[2 * kb + 1] * g[1]));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = 32 * (kb >> 1) + acc_row(8 * (kb & 1) + e, h);
-                x[e] = z.scale * eG[i] * d[kb >> 1][8 * (kb & 1) + e];
-                y[e] = -beta[i] * eG[i] * R[kb >> 1][8 * (kb & 1) + e];
-            }
-            split8(x, o);
-            split8(y, r);
-#pragma unroll
-            for (int t = 0; t < DK / 32; ++t) {
-                S[t] = mma(tile8<X, L::kTok>(Qt, 32 * t, 16 * kb, lane), o, S[t]);
-                S[t] = mma(tile8<X, L::kTok>(Kt, 32 * t, 16 * kb, lane), r, S[t]);
+            for (int t = 0; t < DK / 16; ++t) {
+                S[t] = mma(tile8<X, L::kTok>(Qt, 16 * t, 32 * kb, lane), o, S[t]);
+                S[t] = mma(tile8<X, L::kTok>(Kt, 16 * t, 32 * kb, lane), r, S[t]);
             }
         }
+        if (!kAhead && c > c0) take_columns(c - 1);
     }
     if (active && a.final_state && (!FULL || seg == 0))
-        put_state<DK>(S, a.final_state + bh * a.final_head + (FULL ? 0 : static_cast<size_t>(seg) * z.dk * z.dv), z.dk, z.dv, vcol, h);
+        put_state(S, a.final_state + bh * a.final_head + (FULL ? 0 : static_cast<size_t>(seg) * z.dk * z.dv), z.dk, z.dv, 0, vcol, lane);
 }
 
 // ------------------------------------------------------------------ gradients of a chunk
@@ -774,6 +776,42 @@ struct GradArgs {
     int shared;
     float *dg, *dbeta;
 };
+
+// what the 32 x 32 products of this kernel take: rows row0 + lane % 32 of a tile in LDS, 16 places from k0
+template <class X, int STRIDE>
+__device__ __forceinline__ typename X::Exact tall8(const typename X::E *t, int row0, int k0, int lane)
+{
+    return get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5));
+}
+template <class OPERAND, int STRIDE, class E>
+__device__ __forceinline__ OPERAND tall8s(const E *t, int row0, int k0, int lane)
+{
+    OPERAND x;
+    get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5), C * STRIDE, x);
+    return x;
+}
+// an accumulator of 32 tokens, stored row by row, rounded to the element type
+template <class X>
+__device__ __forceinline__ void store_tall(typename X::E *p, int row0, int rows, int width, int k0, const f32x16 &c, int lane)
+{
+    f32x16 t = zero16();
+#pragma unroll
+    for (int g16 = 0; g16 < 2; ++g16) {
+        float x[8];
+        typename X::Exact s;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = c[8 * g16 + e];
+        round8(x, s);
+        t = mma(s, unit8<X, 32, true>(g16, lane), t);
+    }
+    const int row = row0 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = k0 + 8 * i + 4 * (lane >> 5);
+        const float x[4] = {t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]};
+        if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, x);
+    }
+}
 
 // sums over the 32 lanes of a half of 32 values a lane: afterwards lane l holds the sum of value sum32_index(l)
 __device__ __forceinline__ float sum32(float (&v)[32], int lane)
@@ -791,12 +829,12 @@ __device__ __forceinline__ float sum32(float (&v)[32], int lane)
 }
 __device__ __forceinline__ int sum32_index(int lane) { return lane & 31; }
 
-// rows row0 + lane % 32 of a caller's tensor, 16 elements from k0 in spread order
+// the elements of a caller's row at eight places of the spread order, from place p (a multiple of 8)
 template <class X>
-__device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *p, int row, int rows, int width, int k0, int h)
+__device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *t, int row, int rows, int width, int p)
 {
-    const int k = k0 + 4 * h;
-    return load8_spread(p + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 8 < width);
+    const int k = (p & ~31) + ((p & 31) >> 1);
+    return load8_spread(t + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 16 < width);
 }
 
 template <class X, int DK>
@@ -828,10 +866,12 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
     qd[tid] = 0.f;
     {
         RowsStage<X, DK> ks, qs;
-        ks.take(K, n, z.dk, tid);
-        qs.take(Q, n, z.dk, tid);
-        ks.template put<false, true>(n, z.dk, nullptr, Kt, tid);
-        qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
+        if (tid < 2 * DK) {
+            ks.take(K, n, z.dk, tid);
+            qs.take(Q, n, z.dk, tid);
+            ks.template put<false, true>(n, z.dk, nullptr, Kt, tid);
+            qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
+        }
     }
     __syncthreads();
 
@@ -843,7 +883,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
             float u[8], r[8], v[8];
             kept8(U + i * z.dvp + 8 * o, u);
             kept8(dR + i * z.dvp + 8 * o, r);
-            values8(rows8_spread<X>(V, i, n, z.dv, 16 * (o >> 1), o & 1), v);
+            values8(rows8_spread<X>(V, i, n, z.dv, 8 * o), v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 ud += u[e] * r[e];
@@ -878,7 +918,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
         for (int kb = 0; kb < z.dvp / 16; ++kb) {
             const int k0 = 16 * kb + 8 * h;
             const typename X::Split uj = kept<typename X::Split>(U + (32 * tj + col) * z.dvp + k0);
-            zz = mma(uj, rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb, h), zz);
+            zz = mma(uj, rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb + 8 * h), zz);
             xx = mma(lead(uj), kept<typename X::Pair>(dR + (32 * ti + col) * z.dvp + k0), xx);
         }
         const int i = 32 * ti + col;
@@ -893,12 +933,12 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
                 e8[e] = j < i ? -bs[i] * D * xx[8 * g16 + e] : 0.f;
                 if (j > i) f[e] = 0.f;
             }
-            typename X::Split s;
-            split8(f, s);
-            put8(F + i * L::kTok + 32 * tj + 16 * g16 + 8 * h, L::kSquare, s);
-            typename X::Pair x;
-            split8(e8, x);
-            put8(Es + i * L::kTok + 32 * tj + 16 * g16 + 8 * h, L::kSquare, x);
+#pragma unroll
+            for (int i8 = 0; i8 < 2; ++i8) {
+                const int to = 32 * tj + spread(16 * g16 + 8 * i8 + 4 * h);
+                put4(F + i * L::kTok + to, L::kSquare, f32x4{f[4 * i8], f[4 * i8 + 1], f[4 * i8 + 2], f[4 * i8 + 3]});
+                put4_pair(Es + i * L::kTok + to, L::kSquare, f32x4{e8[4 * i8], e8[4 * i8 + 1], e8[4 * i8 + 2], e8[4 * i8 + 3]});
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int j = 32 * tj + acc_row(8 * g16 + e, h);
@@ -922,7 +962,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
                 const int k0 = 16 * kb + 8 * h;
                 const typename X::Split s = kept<typename X::Split>(S + dcol * z.dvp + k0);
 #pragma unroll
-                for (int ti = 0; ti < 2; ++ti) R[ti] = mma(rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb, h), s, R[ti]);
+                for (int ti = 0; ti < 2; ++ti) R[ti] = mma(rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb + 8 * h), s, R[ti]);
             }
 #pragma unroll
             for (int ti = 0; ti < 2; ++ti)
@@ -930,20 +970,22 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
                 for (int e = 0; e < 16; ++e) R[ti][e] *= z.scale * eG[32 * ti + acc_row(e, h)];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
-                const typename X::Exact k = tile8<X, L::kTok>(Kt, d0, 16 * kb, lane);
+                const typename X::Exact k = tall8<X, L::kTok>(Kt, d0, 16 * kb, lane);
 #pragma unroll
-                for (int ti = kb >> 1; ti < 2; ++ti) R[ti] = mma(tile8s<typename X::Split, L::kTok>(F, 32 * ti, 16 * kb, lane), k, R[ti]);
+                for (int ti = kb >> 1; ti < 2; ++ti) R[ti] = mma(tall8s<typename X::Split, L::kTok>(F, 32 * ti, 16 * kb, lane), k, R[ti]);
             }
             float p[32];
 #pragma unroll
             for (int ti = 0; ti < 2; ++ti)
 #pragma unroll
-                for (int g16 = 0; g16 < 2; ++g16) {
-                    float q[8];
-                    values8(tile8<X, L::kTok>(Qt, d0, 32 * ti + 16 * g16, lane), q);
+                for (int g16 = 0; g16 < 2; ++g16)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) p[16 * ti + 8 * g16 + e] = q[e] * R[ti][8 * g16 + e];
-                }
+                    for (int i8 = 0; i8 < 2; ++i8) {
+                        float q[4];
+                        get4(Qt + dcol * L::kTok + 32 * ti + spread(16 * g16 + 8 * i8 + 4 * h), q);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[16 * ti + 8 * g16 + 4 * i8 + e] = q[e] * R[ti][8 * g16 + 4 * i8 + e];
+                    }
             const float s = sum32(p, lane);
             const int v = sum32_index(lane);
             qd[wave * C + 32 * (v >> 4) + acc_row(v & 15, h)] += s;
@@ -967,18 +1009,18 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
                 }
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
-                const typename X::Exact k = tile8<X, L::kTok>(Kt, d0, 16 * kb, lane), q = tile8<X, L::kTok>(Qt, d0, 16 * kb, lane);
+                const typename X::Exact k = tall8<X, L::kTok>(Kt, d0, 16 * kb, lane), q = tall8<X, L::kTok>(Qt, d0, 16 * kb, lane);
 #pragma unroll
                 for (int ti = 0; ti < 2; ++ti) {
-                    R[ti] = mma(tile8s<typename X::Pair, L::kTok>(Es, 32 * ti, 16 * kb, lane), k, R[ti]);
-                    if (ti <= kb >> 1) R[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ft, 32 * ti, 16 * kb, lane), q, R[ti]);
+                    R[ti] = mma(tall8s<typename X::Pair, L::kTok>(Es, 32 * ti, 16 * kb, lane), k, R[ti]);
+                    if (ti <= kb >> 1) R[ti] = mma(tall8s<typename X::Pair, L::kTok>(Ft, 32 * ti, 16 * kb, lane), q, R[ti]);
                 }
             }
         }
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) {
             if (!a.shared) {
-                store_rows<X>(static_cast<E *>(isq ? a.dQ : a.dK) + qk_row(z, bh, t0) * z.dk, 32 * ti, n, z.dk, d0, R[ti], lane);
+                store_tall<X>(static_cast<E *>(isq ? a.dQ : a.dK) + qk_row(z, bh, t0) * z.dk, 32 * ti, n, z.dk, d0, R[ti], lane);
                 continue;
             }
             const buffer_t out = buffer(static_cast<float *>(isq ? a.dQ : a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
@@ -1129,8 +1171,9 @@ void set_window(const DeltaPlan &p, int w, Sizes *z)
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;                        \
     } while (0)
 
-template <class X, int DK>
+template <class X, int DK, int THREADS>
 struct Passes {
+    static constexpr int kTiles = THREADS / 64;
     static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
     {
         PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), floats(ws, p.off_M), bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
@@ -1162,8 +1205,8 @@ struct Passes {
         a.transitions = 1;
         a.P = ws + p.off_P;
         a.PT = ws + p.off_PT;
-        const dim3 grid((p.dvp / 32 + DK / 32 + 3) / 4, segs, p.BH);
-        DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, kPre>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+        const dim3 grid((p.dvp / 16 + DK / 16 + kTiles - 1) / kTiles, segs, p.BH);
+        DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, THREADS, kPre>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
         return hipSuccess;
     }
     static hipError_t combine(const DeltaPlan &p, const Sizes &z, const float *carry, size_t carry_head, char *ws, int steps, bool rev, hipStream_t st)
@@ -1177,9 +1220,9 @@ struct Passes {
         a.at = floats(ws, rev ? p.off_end : p.off_start);
         a.at_head = static_cast<size_t>(p.dk) * p.dv * (rev ? p.nseg : p.nseg + 1);
         a.steps = steps;
-        const dim3 grid(p.dvp / 32, p.BH);
-        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 2 * DK, 0, st, a);
-        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 2 * DK, 0, st, a);
+        const dim3 grid(p.dvp / 16, p.BH);
+        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 4 * DK, 0, st, a);
+        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 4 * DK, 0, st, a);
         return hipSuccess;
     }
 
@@ -1205,8 +1248,8 @@ struct Passes {
             a.final_state = w + 1 < p.windows ? kept : io.state_out;
             a.final_head = one;
             carry = kept;
-            const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
-            DELTA_LAUNCH("delta_scan", (delta_scan_kernel<X, DK, kOut>), grid, 256, (scan_lds<X, DK>(true)), st, a);
+            const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, z.segs, p.BH);
+            DELTA_LAUNCH("delta_scan", (delta_scan_kernel<X, DK, THREADS, kOut>), grid, THREADS, (scan_lds<X, DK>(true)), st, a);
         }
         return hipSuccess;
     }
@@ -1235,8 +1278,8 @@ struct Passes {
                 a.final_head = one * (p.nseg + 1);
                 carry = a.final_state;
                 if (w + 1 < p.windows) {
-                    const dim3 grid((p.dvp / 32 + 3) / 4, 1, p.BH);
-                    DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, kPre>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+                    const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, 1, p.BH);
+                    DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, THREADS, kPre>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
                 }
             }
         }
@@ -1253,8 +1296,8 @@ struct Passes {
                 a.start_head = own_start ? one * (p.nseg + 1) : one;
                 a.S = floats(ws, p.off_S);
                 a.U = floats(ws, p.off_U);
-                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
-                DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, kKeep>), grid, 256, (scan_lds<X, DK>(false)), st, a);
+                const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, z.segs, p.BH);
+                DELTA_LAUNCH("delta_states", (delta_scan_kernel<X, DK, THREADS, kKeep>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
             }
             RevArgs r{};
             r.z = z;
@@ -1271,8 +1314,8 @@ struct Passes {
                 r.final_state = floats(ws, p.off_add) + z.seg0 * one;
                 r.final_head = one * p.nseg;
                 r.seg_skip = 1;
-                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs - 1, p.BH);
-                DELTA_LAUNCH("delta_segments_back", (delta_rev_kernel<X, DK, false>), grid, 256, (rev_lds<X, DK>()), st, r);
+                const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, z.segs - 1, p.BH);
+                DELTA_LAUNCH("delta_segments_back", (delta_rev_kernel<X, DK, THREADS, false>), grid, THREADS, (rev_lds<X, DK>()), st, r);
                 if (hipError_t e = combine(p, z, dcarry, one, ws, z.segs - 1, true, st); e != hipSuccess) return e;
                 full.end = end + z.seg0 * one;
                 full.end_head = one * p.nseg;
@@ -1284,8 +1327,8 @@ struct Passes {
             full.dR = floats(ws, p.off_dR);
             dcarry = kept;
             {
-                const dim3 grid((p.dvp / 32 + 3) / 4, z.segs, p.BH);
-                DELTA_LAUNCH("delta_scan_back", (delta_rev_kernel<X, DK, true>), grid, 256, (rev_lds<X, DK>()), st, full);
+                const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, z.segs, p.BH);
+                DELTA_LAUNCH("delta_scan_back", (delta_rev_kernel<X, DK, THREADS, true>), grid, THREADS, (rev_lds<X, DK>()), st, full);
             }
             const float *a_S = floats(ws, p.off_S), *a_U = floats(ws, p.off_U);
             const bool shared = p.H != p.Hk;
@@ -1303,12 +1346,15 @@ struct Passes {
     }
 };
 
-template <class F>
-hipError_t for_shape(const DeltaPlan &p, F f)
+// Eight wavefronts where there are columns or rows for them: a workgroup of four has half the tiles to stage and fits a CU twice.
+template <class X, class F>
+hipError_t for_width(const DeltaPlan &p, F f)
 {
-    if (p.dtype == RACE_BF16) return p.dk <= 64 ? f(Passes<Bf, 64>()) : f(Passes<Bf, 128>());
-    return p.dk <= 64 ? f(Passes<Fp, 64>()) : f(Passes<Fp, 128>());
+    if (p.dk > 64) return f(Passes<X, 128, 512>());
+    return p.dvp > 64 ? f(Passes<X, 64, 512>()) : f(Passes<X, 64, 256>());
 }
+template <class F>
+hipError_t for_shape(const DeltaPlan &p, F f) { return p.dtype == RACE_BF16 ? for_width<Bf>(p, f) : for_width<Fp>(p, f); }
 
 __global__ __launch_bounds__(256) void delta_copy_state_kernel(const float *from, float *to, size_t n)
 {
