@@ -72,6 +72,10 @@ struct Fp {
     static constexpr int kPad = 4;
 };
 
+// The wavefront's number as a scalar.  Branches on it have to be scalar branches: matrix instructions do not look at EXEC, and
+// in a region that the compiler takes for divergent they are also run by wavefronts that have no lane in it.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)); }
+
 __device__ __forceinline__ f32x16 zero16()
 {
     f32x16 z;

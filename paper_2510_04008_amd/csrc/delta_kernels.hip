@@ -52,13 +52,6 @@ __device__ __forceinline__ OPERAND kept(const float *p)
     return s;
 }
 
-// a half of a 32 x 32 accumulator (8 rows: k, k + 1, .. and k + 8, ..) into a row of an image
-__device__ __forceinline__ void keep8(float *row, int k, const float *x)
-{
-    *reinterpret_cast<f32x4 *>(row + spread(k)) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4 *>(row + spread(k + 8)) = f32x4{x[4], x[5], x[6], x[7]};
-}
-
 // ------------------------------------------------------------------ what a chunk needs besides the states
 // T, M and the decays of one chunk of one head.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane per
 // column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions.  Substitution and not powers of A: with keys alike the powers
@@ -95,7 +88,7 @@ struct PrepArgs {
     Sizes z;
     const void *Q, *K;
     const float *g, *beta;
-    float *T, *M;           // 64 x 64 each, rows in spread order; backward: also T^T, and M^T in M's place
+    void *T, *M;            // 64 x 64 images, rows in spread order: T - I and M (Pairs); backward: M^T in M's place, and T^T - I (fp32)
     float *TT;
     float *dec;             // per chunk: e^G, e^{G_C - G}, beta
 };
@@ -108,7 +101,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     __shared__ float B[C];
     __shared__ __attribute__((aligned(16))) float A[C][68], T[C][68];
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, h = lane >> 5, col = lane & 31;
     const int bh = blockIdx.y, n = tokens_of(z, z.chunk0 + blockIdx.x);
     const int64_t t0 = static_cast<int64_t>(z.chunk0 + blockIdx.x) * C;
     const size_t at = static_cast<size_t>(bh) * z.chunks + blockIdx.x;
@@ -137,7 +130,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
             kk = mma(ki, kj, kk);
             qk = BWD ? mma(qi, kj, qk) : mma(kj, qi, qk);       // the image's row is the accumulator's column
         }
-        float *M = a.M + at * C * C;
+        E *M = static_cast<E *>(a.M) + at * X::kPairPlanes * C * C;
+        float *MT = static_cast<float *>(a.M) + at * C * C;
 #pragma unroll
         for (int g16 = 0; g16 < 2; ++g16) {
             float m[8];
@@ -147,7 +141,13 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
                 const int i = 32 * ti + (BWD ? row : col), j = 32 * tj + (BWD ? col : row);
                 m[e] = j <= i ? z.scale * expf(static_cast<float>(G[i] - G[j])) * qk[8 * g16 + e] : 0.f;
             }
-            keep8(M + (BWD ? (32 * tj + col) * C + 32 * ti : (32 * ti + col) * C + 32 * tj), 16 * g16 + 4 * h, m);
+#pragma unroll
+            for (int i8 = 0; i8 < 2; ++i8) {
+                const f32x4 v = {m[4 * i8], m[4 * i8 + 1], m[4 * i8 + 2], m[4 * i8 + 3]};
+                const int k = spread(16 * g16 + 8 * i8 + 4 * h);
+                if (BWD) *reinterpret_cast<f32x4 *>(MT + (32 * tj + col) * C + 32 * ti + k) = v;
+                else put4_pair(M + (32 * ti + col) * C + 32 * tj + k, C * C, v);
+            }
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -176,8 +176,15 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     __syncthreads();
     for (int task = tid; task < C * 16; task += 256) {
         const int row = task >> 4, k = 4 * (task & 15);
-        *reinterpret_cast<f32x4 *>(a.T + at * C * C + row * C + spread(k)) = *reinterpret_cast<const f32x4 *>(&T[row][k]);
-        if (BWD) *reinterpret_cast<f32x4 *>(a.TT + at * C * C + row * C + spread(k)) = f32x4{T[k][row], T[k + 1][row], T[k + 2][row], T[k + 3][row]};
+        const size_t to = at * X::kPairPlanes * C * C + row * C + spread(k);
+        f32x4 v, w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = k + e == row ? 0.f : T[row][k + e];
+            w[e] = k + e == row ? 0.f : T[k + e][row];
+        }
+        put4_pair(static_cast<E *>(a.T) + to, C * C, v);
+        if (BWD) *reinterpret_cast<f32x4 *>(a.TT + at * C * C + row * C + spread(k)) = w;
     }
 }
 
@@ -185,49 +192,49 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
 template <class X, int DK>
 struct Lds {
     typedef typename X::E E;
-    static constexpr int kRow = DK + X::kPad;       // a token's row, spread over k
+    static constexpr int kRow = DK + X::kPad;       // a token's row
     static constexpr int kTok = C + X::kPad;        // a row over tokens, in spread order
     static constexpr int kByTokens = C * kRow, kByRows = DK * kTok, kSquare = C * kTok;
 };
 
 // 64 rows of a caller's tensor on their way into LDS, as they are, or transposed, or both.  Loads are asked for a chunk ahead (take) and
 // written when the tiles are free (put): with two wavefronts per SIMD nothing else hides their latency.  2 DK tasks of four tokens by eight elements.
+// The rows of the transposed tile are stored in the order of the state's rows in the accumulators (row_place).
+__device__ __forceinline__ int row_place(int k) { return (k & ~31) | ((k & 4) << 2) | ((k & 24) >> 1) | (k & 3); }
 template <class X, int DK>
 struct RowsStage {
     typedef typename X::E E;
     typedef Lds<X, DK> L;
     typename X::Exact x[4];
+    // sixteen lanes take four by four: neither way of writing meets one bank more than twice
+    static __device__ __forceinline__ int quad(int task) { return (task & 3) | (task >> 2 & 12); }
+    static __device__ __forceinline__ int octet(int task) { return (task >> 2 & 3) | (task >> 4 & ~3); }
     __device__ __forceinline__ void take(const E *src, int n, int dk, int task)
     {
-        const int tq = task & 15, o = task >> 4;
+        const int tq = quad(task), o = octet(task);
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = load8(src + static_cast<int64_t>(min(4 * tq + r, n - 1)) * dk + (8 * o < dk ? 8 * o : 0), true);
     }
-    template <bool ROWS, bool COLS>
+    template <bool ROWS, bool COLS, bool PLACED = true>
     __device__ __forceinline__ void put(int n, int dk, E *rows, E *cols, int task)
     {
-        const int tq = task & 15, o = task >> 4;
+        const int tq = quad(task), o = octet(task);
         if (n < C || dk < DK) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = or_zero(x[r], 4 * tq + r < n && 8 * o < dk);
         }
-        E e[4][8];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) __builtin_memcpy(e[r], &x[r], sizeof e[r]);
         if (ROWS) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    E *to = rows + (4 * tq + r) * L::kRow + spread(8 * o + 4 * i);
-                    __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), &e[r][4 * i], 4 * sizeof(E));
-                }
+            for (int r = 0; r < 4; ++r) put8(rows + (4 * tq + r) * L::kRow + 8 * o, x[r]);
         }
         if (COLS) {
+            E e[4][8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) __builtin_memcpy(e[r], &x[r], sizeof e[r]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 E v[4] = {e[0][k], e[1][k], e[2][k], e[3][k]};
-                E *to = cols + (8 * o + k) * L::kTok + spread(4 * tq);
+                E *to = cols + (PLACED ? row_place(8 * o + k) : 8 * o + k) * L::kTok + spread(4 * tq);
                 __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(E)), v, 4 * sizeof(E));
             }
         }
@@ -254,6 +261,28 @@ struct ImageStage {
             OPERAND s;
             split8(x[i], s);
             put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, s);
+        }
+    }
+};
+
+// a 64 x 64 image of Pairs on its way into LDS
+template <int THREADS>
+struct PairStage {
+    static constexpr int kEach = 1024 / THREADS;
+    u32x4 x[kEach];
+    __device__ __forceinline__ void take(const void *src, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[i] = static_cast<const u32x4 *>(src)[tid + THREADS * i];
+    }
+    template <class X>
+    __device__ __forceinline__ void put(typename X::E *dst, int tid) const
+    {
+        constexpr int kTok = C + X::kPad, kPer = 16 / sizeof(typename X::E);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = (tid + THREADS * i) * kPer;      // planes behind one another: rows of one tile of 64 or 128 rows
+            *reinterpret_cast<u32x4 *>(dst + at / C * kTok + at % C) = x[i];
         }
     }
 };
@@ -303,12 +332,12 @@ struct ColumnsStage {
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) x[ti] = load8(p + static_cast<int64_t>(min(16 * ti + (lane & 15), n - 1)) * width + (k < width ? k : 0), true);
     }
-    // (selected without a branch: behind one, the compiler has read the product's accumulators before they were there)
-    __device__ __forceinline__ f32x4 tile(int ti, int n, int width, int k0, int lane) const
+    // Rows behind the last token repeat it: their strengths are 1e-18 and their keys and queries zero.  Columns that there are not are zeros of `unit`.
+    static __device__ __forceinline__ typename X::Exact unit(int width, int k0, int lane)
     {
-        const bool there = lane < 32 && 16 * ti + (lane & 15) < n && k0 + 8 * ((lane >> 4) & 1) < width;
-        return mma(or_zero(x[ti], there), unit8<X, 16, false>(0, lane), zero4());
+        return or_zero(unit8<X, 16, false>(0, lane), k0 + 8 * ((lane >> 4) & 1) < width);
     }
+    __device__ __forceinline__ f32x4 tile(int ti, const typename X::Exact &unit) const { return mma(x[ti], unit, zero4()); }
 };
 // the way back, rounded to the element type: two accumulators on top of one another, 32 rows from row0
 template <class X>
@@ -324,35 +353,38 @@ __device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows,
         if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, y);
     }
 }
-// two accumulators on top of one another into an image of the workspace, 32 rows from row0, columns k0 .. k0 + 15 in spread order
-template <class X>
+// Two accumulators on top of one another into an image of the workspace, 32 rows from row0, columns k0 .. k0 + 15 in spread order.  STATE: rows dealt as
+// the state's.
+template <class X, bool STATE>
 __device__ __forceinline__ void keep_rows(float *p, int row0, int width, int k0, const f32x4 &first, const f32x4 &second, int lane)
 {
     const typename X::Split x = operand<typename X::Split>(first, second);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
-        *reinterpret_cast<f32x4 *>(p + (row0 + 16 * b + (lane & 15)) * width + spread(k0 + 4 * (lane >> 4))) = mma(x, unit8<X, 16, true>(b, lane), zero4());
+        *reinterpret_cast<f32x4 *>(p + (row0 + 16 * b + (lane & 15)) * width + spread(k0 + 4 * (lane >> 4))) = mma(x, unit8<X, 16, !STATE>(b, lane), zero4());
 }
 
-// a wavefront's 16 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written
+// A wavefront's 16 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written.  Rows are
+// dealt to the accumulators so that two of them, as an operand, hold rows 8 q .. 8 q + 7 of 32 (the order of K's rows in memory).
+__device__ __forceinline__ int state_row(int tile, int q, int e) { return 32 * (tile >> 1) + 8 * q + 4 * (tile & 1) + e; }
 __device__ __forceinline__ int state_offset(int row, int dv, int col) { return col < dv ? 4 * (row * dv + col) : kNowhere; }
 template <int TILES>
-__device__ __forceinline__ void get_state(f32x4 (&S)[TILES], const float *state, int dk, int dv, int row0, int col, int lane)
+__device__ __forceinline__ void get_state(f32x4 (&S)[TILES], const float *state, int dk, int dv, int tile0, int col, int lane)
 {
     const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[t][e] = get_buffer(b, state_offset(row0 + 16 * t + 4 * (lane >> 4) + e, dv, col));
+        for (int e = 0; e < 4; ++e) S[t][e] = get_buffer(b, state_offset(state_row(tile0 + t, lane >> 4, e), dv, col));
 }
 template <int TILES>
-__device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state, int dk, int dv, int row0, int col, int lane)
+__device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state, int dk, int dv, int tile0, int col, int lane)
 {
     const buffer_t b = buffer(state, static_cast<size_t>(dk) * dv);
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) put_buffer(b, state_offset(row0 + 16 * t + 4 * (lane >> 4) + e, dv, col), S[t][e]);
+        for (int e = 0; e < 4; ++e) put_buffer(b, state_offset(state_row(tile0 + t, lane >> 4, e), dv, col), S[t][e]);
 }
 
 // ------------------------------------------------------------------ the states, chunk after chunk
@@ -363,8 +395,8 @@ enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's tran
 
 struct ScanArgs {
     Sizes z;
-    const void *Q, *K, *V;
-    const float *T, *M, *dec;
+    const void *Q, *K, *V, *T, *M;
+    const float *dec;
     const float *start;             // state at the start of a segment, (dk, dv) fp32: start + bh * start_head + segment * dk * dv; null: zero
     size_t start_head;
     float *final_state;             // state behind the window's last segment (null: not wanted); kPre: behind every segment
@@ -380,13 +412,14 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 {
     typedef typename X::E E;
     typedef typename X::Split Split;
+    typedef typename X::Pair Pair;
     typedef Lds<X, DK> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPlanes * L::kSquare;
+    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPairPlanes * L::kSquare;
     E *Ms = Qs + L::kByTokens;
     float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPairPlanes * L::kSquare : Qs);
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4, col = lane & 15;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, q = lane >> 4, col = lane & 15;
     const int bh = blockIdx.z, seg = blockIdx.y;
     const int vtiles = z.dvp / 16, tile = blockIdx.x * (THREADS / 64) + wave;
     const bool trans = MODE == kPre && tile >= vtiles;
@@ -404,14 +437,15 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 #pragma unroll
         for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[t][e] = 16 * t + 4 * q + e == vcol - z.dvp ? 1.f : 0.f;
+            for (int e = 0; e < 4; ++e) S[t][e] = state_row(t, q, e) == vcol - z.dvp ? 1.f : 0.f;
     } else if (a.start && active) {
         get_state(S, a.start + bh * a.start_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, 0, vcol, lane);
     }
     constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
     RowsStage<X, DK> rows;
-    ImageStage<THREADS> is, ms;
+    PairStage<THREADS> is, ms;
     ColumnsStage<X> vs;
+    const typename X::Exact unit = ColumnsStage<X>::unit(z.dv, 16 * tile, lane);
     float ds = 0.f;
     auto take = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -419,8 +453,8 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
         if (kAhead) {
-            is.take(a.T + at * C * C, tid);
-            if (MODE == kOut) ms.take(a.M + at * C * C, tid);
+            is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
+            if (MODE == kOut) ms.take(static_cast<const E *>(a.M) + at * X::kPairPlanes * C * C, tid);
         }
         if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
     };
@@ -439,11 +473,11 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         __syncthreads();
         if (has_k) rows.template put<true, true>(n, z.dk, Ks, Kt, task);
         if (has_q) rows.template put<true, false>(n, z.dk, Qs, nullptr, task);
-        if (!kAhead) is.take(a.T + at * C * C, tid);
-        is.template put<X, Split>(Ts, tid);
+        if (!kAhead) is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
+        is.template put<X>(Ts, tid);
         if (MODE == kOut) {
-            if (!kAhead) ms.take(a.M + at * C * C, tid);
-            ms.template put<X, typename X::Pair>(Ms, tid);
+            if (!kAhead) ms.take(static_cast<const E *>(a.M) + at * X::kPairPlanes * C * C, tid);
+            ms.template put<X>(Ms, tid);
         }
         if (tid < 3 * C) dec[tid] = ds;
         __syncthreads();
@@ -453,7 +487,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (MODE == kKeep) {
             float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp;
 #pragma unroll
-            for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
+            for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
         }
         fence();
         // K S, and Q S for the outputs
@@ -475,7 +509,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) {
             f32x4 v = zero4();
-            if (MODE != kPre || !trans) v = vs.tile(ti, n, z.dv, 16 * tile, lane);
+            if (MODE != kPre || !trans) v = vs.tile(ti, unit);
             const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + 16 * ti + 4 * q), b = *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -485,31 +519,31 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         }
         if (c + 1 < c1) take_columns(c + 1);
         fence();
-        // U = T R, and the outputs' M U
+        // U = T R = R + (T - I) R, and the outputs' M U
         f32x4 U[4];
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) U[ti] = zero4();
+        for (int ti = 0; ti < 4; ++ti) U[ti] = R[ti];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const Split r = operand<Split>(R[2 * kb], R[2 * kb + 1]);
+            const Pair r = operand<Pair>(R[2 * kb], R[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
 #pragma unroll
-            for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
+            for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Pair, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
         }
         if (MODE == kOut) {
             E *out = static_cast<E *>(a.O) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const typename X::Pair u = operand<typename X::Pair>(U[2 * kb], U[2 * kb + 1]);
+                const Pair u = operand<Pair>(U[2 * kb], U[2 * kb + 1]);
 #pragma unroll
-                for (int ti = 2 * kb; ti < 4; ++ti) O[ti] = mma(tile8s<typename X::Pair, L::kTok>(Ms, 16 * ti, 32 * kb, lane), u, O[ti]);
+                for (int ti = 2 * kb; ti < 4; ++ti) O[ti] = mma(tile8s<Pair, L::kTok>(Ms, 16 * ti, 32 * kb, lane), u, O[ti]);
                 store_rows<X>(out, 32 * kb, n, z.dv, 16 * tile, O[2 * kb], O[2 * kb + 1], lane);
             }
         }
         if (MODE == kKeep) {
             float *keep = a.U + at * C * z.dvp;
 #pragma unroll
-            for (int ti = 0; ti < 4; ti += 2) keep_rows<X>(keep, 16 * ti, z.dvp, 16 * tile, U[ti], U[ti + 1], lane);
+            for (int ti = 0; ti < 4; ti += 2) keep_rows<X, false>(keep, 16 * ti, z.dvp, 16 * tile, U[ti], U[ti + 1], lane);
         }
         fence();
         // the state behind the chunk
@@ -529,10 +563,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     if (MODE == kKeep && c1 == z.chunks) {
         float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
 #pragma unroll
-        for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
+        for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
     }
     if (trans) {
-        // P as a left operand: rows of the accumulators, its columns spread; P^T: the columns, whose rows are a lane's eight values
+        // P as a left operand, row by row; P^T: its columns, of which a lane holds eight rows that lie together
         E *P = static_cast<E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
         E *PT = static_cast<E *>(a.PT) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
         const int k0 = 16 * tile - z.dvp;
@@ -542,8 +576,8 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
             put8(PT + (k0 + col) * DK + 16 * t + 8 * q, DK * DK, x);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const f32x4 y = mma(x, unit8<X, 16, true>(b, lane), zero4());
-                put4(P + (16 * t + 16 * b + col) * DK + spread(k0 + 4 * q), DK * DK, y);
+                const f32x4 y = mma(x, unit8<X, 16, false>(b, lane), zero4());
+                put4(P + (16 * t + 16 * b + col) * DK + k0 + 4 * q, DK * DK, y);
             }
         }
         return;
@@ -574,22 +608,22 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     typedef typename X::Split Split;
     __shared__ __attribute__((aligned(16))) E ops[2][X::kPlanes][DK / 32][64 * 8];
     const Sizes &z = a.z;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane >> 4, col = 16 * blockIdx.x + (lane & 15), bh = blockIdx.y;
+    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * blockIdx.x + (lane & 15), bh = blockIdx.y;
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
     auto segment = [&](int i) { return REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i; };
     Split P[DK / 32];
     f32x4 B[1], S[1] = {zero4()};
     auto take = [&](int i) {
         const size_t s = static_cast<size_t>(bh) * z.nseg + segment(i);
-        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + (16 * wave + (lane & 15)) * DK + 8 * q;
+        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + state_row(wave, lane >> 2 & 3, lane & 3) * DK + 8 * q;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, P[kb]);
-        get_state(B, a.add + s * one, z.dk, z.dv, 16 * wave, col, lane);
+        get_state(B, a.add + s * one, z.dk, z.dv, wave, col, lane);
     };
-    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, 16 * wave, col, lane);
+    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, wave, col, lane);
     if (a.steps > 0) take(0);
     for (int i = 0; i <= a.steps; ++i) {
-        put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, 16 * wave, col, lane);
+        put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane);
         if (i == a.steps) break;
         // the lane's four rows are half of its eight places in the operand of 32 rows
         put4(&ops[i & 1][0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[0]);
@@ -635,7 +669,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
     E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Qt = Kt + L::kByRows, *Ts = Qt + L::kByRows, *Ms = Ts + X::kPlanes * L::kSquare;
     float *dec = reinterpret_cast<float *>(Ms + X::kPlanes * L::kSquare);
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, q = lane >> 4;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, q = lane >> 4;
     const int bh = blockIdx.z, seg = blockIdx.y + a.seg_skip;
     const int tile = blockIdx.x * (THREADS / 64) + wave, vcol = 16 * tile + (lane & 15);
     const bool active = tile < z.dvp / 16;
@@ -652,6 +686,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
     RowsStage<X, DK> rows;
     ImageStage<THREADS> is, ms;
     ColumnsStage<X> os;
+    const typename X::Exact unit = ColumnsStage<X>::unit(z.dv, 16 * tile, lane);
     float ds = 0.f;
     auto take = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -691,11 +726,11 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         if (FULL) {
             float *keep = a.dS + at * DK * z.dvp;
 #pragma unroll
-            for (int t = 0; t < DK / 16; t += 2) keep_rows<X>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
+            for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
         }
         f32x4 d[4];
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) d[ti] = os.tile(ti, n, z.dv, 16 * tile, lane);
+        for (int ti = 0; ti < 4; ++ti) d[ti] = os.tile(ti, unit);
         if (kAhead && c > c0) take_columns(c - 1);
         fence();
         // dU = M^T dO + e^{G_C - G} K dS
@@ -718,10 +753,10 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
             for (int ti = 0; ti < 2 * kb + 2; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ms, 16 * ti, 32 * kb, lane), o, U[ti]);
         }
         fence();
-        // dR = T^T dU
+        // dR = T^T dU = dU + (T^T - I) dU
         f32x4 R[4];
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) R[ti] = zero4();
+        for (int ti = 0; ti < 4; ++ti) R[ti] = U[ti];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const Split u = operand<Split>(U[2 * kb], U[2 * kb + 1]);
@@ -737,7 +772,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
             E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int ti = 0; ti < 4; ti += 2) {
-                keep_rows<X>(keep, 16 * ti, z.dvp, 16 * tile, R[ti], R[ti + 1], lane);
+                keep_rows<X, false>(keep, 16 * ti, z.dvp, 16 * tile, R[ti], R[ti + 1], lane);
                 store_rows<X>(dV, 16 * ti, n, z.dv, 16 * tile, b[ti] * R[ti], b[ti + 1] * R[ti + 1], lane);
             }
         }
@@ -847,7 +882,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
     float *eG = reinterpret_cast<float *>(G + C), *eEnd = eG + C, *bs = eEnd + C, *qd = bs + C /* 4 C */, *vd = qd + 4 * C, *part = vd + C /* 8 */;
     E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *F = Qt + L::kByRows, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, h = lane >> 5, col = lane & 31;
     const int bh = blockIdx.y, c = blockIdx.x, n = tokens_of(z, z.chunk0 + c);
     const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
     const size_t at = static_cast<size_t>(bh) * z.chunks + c;
@@ -869,8 +904,8 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
         if (tid < 2 * DK) {
             ks.take(K, n, z.dk, tid);
             qs.take(Q, n, z.dk, tid);
-            ks.template put<false, true>(n, z.dk, nullptr, Kt, tid);
-            qs.template put<false, true>(n, z.dk, nullptr, Qt, tid);
+            ks.template put<false, true, false>(n, z.dk, nullptr, Kt, tid);
+            qs.template put<false, true, false>(n, z.dk, nullptr, Qt, tid);
         }
     }
     __syncthreads();
@@ -1124,7 +1159,7 @@ template <class X, int DK>
 constexpr size_t scan_lds(bool out)
 {
     typedef Lds<X, DK> L;
-    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + 3 * C * sizeof(float);
+    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPairPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + 3 * C * sizeof(float);
 }
 template <class X, int DK>
 constexpr size_t rev_lds()
@@ -1176,7 +1211,7 @@ struct Passes {
     static constexpr int kTiles = THREADS / 64;
     static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
     {
-        PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), floats(ws, p.off_M), bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
+        PrepArgs a{z, io.Q, io.K, io.g, io.beta, ws + p.off_T, ws + p.off_M, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
         const dim3 grid(z.chunks, p.BH);
         if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
         else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
@@ -1189,8 +1224,8 @@ struct Passes {
         a.Q = io.Q;
         a.K = io.K;
         a.V = io.V;
-        a.T = floats(ws, p.off_T);
-        a.M = floats(ws, p.off_M);
+        a.T = ws + p.off_T;
+        a.M = ws + p.off_M;
         a.dec = floats(ws, p.off_dec);
         return a;
     }
