@@ -261,19 +261,19 @@ __device__ __forceinline__ Fp::Exact load8(const float *p, bool there)
     return x;
 }
 
-// The unit matrix as a right operand, its row 16 b + n in column n (16 columns, natural or spread; 32 columns, spread).  A product with it turns an
+// The unit matrix as a right operand, its row 16 b + n in column n (16 columns, natural or spread).  A product with it turns an
 // operand whose lanes hold rows into an accumulator whose lanes hold columns, exactly (every value times one, plus zeros): rows that lie together in memory become
 // accumulators, and accumulators rows that are stored 8 or 16 bytes at a time, without a way through LDS.
-template <class X, int WIDTH, bool SPREAD>
+template <class X, bool SPREAD>
 __device__ __forceinline__ typename X::Exact unit8(int b, int lane)
 {
     float x[8];
     typename X::Exact u;
+    if (sizeof(u) == 32) asm volatile("" : "+v"(lane));     // fp32: made anew each time, not kept in registers
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int part = lane / WIDTH;      // q or h
-        const int k = !SPREAD ? 8 * part + j : WIDTH == 16 ? 16 * (j >> 2) + 4 * part + (j & 3) : 16 * b + 8 * (j >> 2) + 4 * part + (j & 3);
-        x[j] = (WIDTH == 16 ? k - 16 * b : k) == lane % WIDTH ? 1.f : 0.f;
+        const int q = lane >> 4, k = SPREAD ? 16 * (j >> 2) + 4 * q + (j & 3) : 8 * q + j;
+        x[j] = k - 16 * b == (lane & 15) ? 1.f : 0.f;
     }
     round8(x, u);
     return u;
@@ -288,6 +288,8 @@ __device__ __forceinline__ buffer_t buffer(const float *p, size_t floats)
 }
 __device__ __forceinline__ float get_buffer(buffer_t b, int offset) { return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0)); }
 __device__ __forceinline__ void put_buffer(buffer_t b, int offset, float x) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), b, offset, 0, 0); }
+
+__device__ __forceinline__ void put_buffer(buffer_t b, int offset, const f32x4 &x) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), b, offset, 0, 0); }
 
 // four elements of a caller's row
 __device__ __forceinline__ void store4(uint16_t *p, const float *x)

@@ -335,7 +335,7 @@ struct ColumnsStage {
     // Rows behind the last token repeat it: their strengths are 1e-18 and their keys and queries zero.  Columns that there are not are zeros of `unit`.
     static __device__ __forceinline__ typename X::Exact unit(int width, int k0, int lane)
     {
-        return or_zero(unit8<X, 16, false>(0, lane), k0 + 8 * ((lane >> 4) & 1) < width);
+        return or_zero(unit8<X, false>(0, lane), k0 + 8 * ((lane >> 4) & 1) < width);
     }
     __device__ __forceinline__ f32x4 tile(int ti, const typename X::Exact &unit) const { return mma(x[ti], unit, zero4()); }
 };
@@ -347,21 +347,21 @@ __device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows,
     const int k = k0 + 4 * (lane >> 4);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        const f32x4 t = mma(x, unit8<X, 16, true>(b, lane), zero4());
+        const f32x4 t = mma(x, unit8<X, true>(b, lane), zero4());
         const int row = row0 + 16 * b + (lane & 15);
         const float y[4] = {t[0], t[1], t[2], t[3]};
         if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, y);
     }
 }
-// Two accumulators on top of one another into an image of the workspace, 32 rows from row0, columns k0 .. k0 + 15 in spread order.  STATE: rows dealt as
-// the state's.
+// Two accumulators on top of one another, as the operand that they are, into an image of the workspace: 32 rows from row0, columns k0 .. k0 + 15 in
+// spread order.  STATE: rows dealt as the state's.
 template <class X, bool STATE>
-__device__ __forceinline__ void keep_rows(float *p, int row0, int width, int k0, const f32x4 &first, const f32x4 &second, int lane)
+__device__ __forceinline__ void keep_rows(float *p, int rows, int row0, int width, int k0, const typename X::Split &x, int lane)
 {
-    const typename X::Split x = operand<typename X::Split>(first, second);
+    const buffer_t image = buffer(p, static_cast<size_t>(rows) * width);
+    const int to = 4 * ((lane & 15) * width + spread(k0 + 4 * (lane >> 4)));
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-        *reinterpret_cast<f32x4 *>(p + (row0 + 16 * b + (lane & 15)) * width + spread(k0 + 4 * (lane >> 4))) = mma(x, unit8<X, 16, !STATE>(b, lane), zero4());
+    for (int b = 0; b < 2; ++b) put_buffer(image, to + 4 * (row0 + 16 * b) * width, mma(x, unit8<X, !STATE>(b, lane), zero4()));
 }
 
 // A wavefront's 16 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written.  Rows are
@@ -484,11 +484,6 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (c + 1 < c1) take(c + 1);
         if (!active) continue;
         const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
-        if (MODE == kKeep) {
-            float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp;
-#pragma unroll
-            for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
-        }
         fence();
         // K S, and Q S for the outputs
         f32x4 R[4], O[4];
@@ -498,6 +493,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         for (int kb = 0; kb < DK / 32; ++kb) {
             const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
+            if (MODE == kKeep) keep_rows<X, true>(a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, DK, 32 * kb, z.dvp, 16 * tile, s, lane);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
                 R[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, R[ti]);
@@ -543,7 +539,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (MODE == kKeep) {
             float *keep = a.U + at * C * z.dvp;
 #pragma unroll
-            for (int ti = 0; ti < 4; ti += 2) keep_rows<X, false>(keep, 16 * ti, z.dvp, 16 * tile, U[ti], U[ti + 1], lane);
+            for (int ti = 0; ti < 4; ti += 2) keep_rows<X, false>(keep, C, 16 * ti, z.dvp, 16 * tile, operand<Split>(U[ti], U[ti + 1]), lane);
         }
         fence();
         // the state behind the chunk
@@ -563,7 +559,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     if (MODE == kKeep && c1 == z.chunks) {
         float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
 #pragma unroll
-        for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
+        for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, DK, 16 * t, z.dvp, 16 * tile, operand<Split>(S[t], S[t + 1]), lane);
     }
     if (trans) {
         // P as a left operand, row by row; P^T: its columns, of which a lane holds eight rows that lie together
@@ -576,7 +572,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
             put8(PT + (k0 + col) * DK + 16 * t + 8 * q, DK * DK, x);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const f32x4 y = mma(x, unit8<X, 16, false>(b, lane), zero4());
+                const f32x4 y = mma(x, unit8<X, false>(b, lane), zero4());
                 put4(P + (16 * t + 16 * b + col) * DK + k0 + 4 * q, DK * DK, y);
             }
         }
@@ -682,7 +678,8 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 #pragma unroll
     for (int t = 0; t < DK / 16; ++t) S[t] = zero4();
     if (a.end && active) get_state(S, a.end + bh * a.end_head + static_cast<size_t>(seg) * z.dk * z.dv, z.dk, z.dv, 0, vcol, lane);
-    constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
+    constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images, at dk > 64 not for rows either
+    constexpr bool kAheadRows = kAhead || DK <= 64;
     RowsStage<X, DK> rows;
     ImageStage<THREADS> is, ms;
     ColumnsStage<X> os;
@@ -692,7 +689,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
-        if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
+        if (kAheadRows && (has_k || has_q)) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
         if (kAhead) {
             is.take(a.TT + at * C * C, tid);
             ms.take(a.MT + at * C * C, tid);
@@ -712,6 +709,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         const int n = tokens_of(z, z.chunk0 + c);
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         __syncthreads();
+        if (!kAheadRows && (has_k || has_q)) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
         if (has_k) rows.template put<true, true>(n, z.dk, Ks, Kt, task);
         if (has_q) rows.template put<false, true>(n, z.dk, nullptr, Qt, task);
         if (!kAhead) is.take(a.TT + at * C * C, tid);
@@ -723,11 +721,6 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         if (c > c0) take(c - 1);
         if (!active) continue;
         const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
-        if (FULL) {
-            float *keep = a.dS + at * DK * z.dvp;
-#pragma unroll
-            for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, 16 * t, z.dvp, 16 * tile, S[t], S[t + 1], lane);
-        }
         f32x4 d[4];
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) d[ti] = os.tile(ti, unit);
@@ -741,6 +734,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         for (int kb = 0; kb < DK / 32; ++kb) {
             const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
+            if (FULL) keep_rows<X, true>(a.dS + at * DK * z.dvp, DK, 32 * kb, z.dvp, 16 * tile, s, lane);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) U[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, U[ti]);
         }
@@ -764,16 +758,14 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 #pragma unroll
             for (int ti = 0; ti < 2 * kb + 2; ++ti) R[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), u, R[ti]);
         }
-        f32x4 b[4];
-#pragma unroll
-        for (int ti = 0; ti < 4; ++ti) b[ti] = *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q);
+        auto strengths = [&](int ti) { return *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q); };
         if (FULL) {
             float *keep = a.dR + at * C * z.dvp;
             E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int ti = 0; ti < 4; ti += 2) {
-                keep_rows<X, false>(keep, 16 * ti, z.dvp, 16 * tile, R[ti], R[ti + 1], lane);
-                store_rows<X>(dV, 16 * ti, n, z.dv, 16 * tile, b[ti] * R[ti], b[ti + 1] * R[ti + 1], lane);
+                keep_rows<X, false>(keep, C, 16 * ti, z.dvp, 16 * tile, operand<Split>(R[ti], R[ti + 1]), lane);
+                store_rows<X>(dV, 16 * ti, n, z.dv, 16 * tile, strengths(ti) * R[ti], strengths(ti + 1) * R[ti + 1], lane);
             }
         }
         fence();
@@ -787,13 +779,13 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 #pragma unroll
             for (int i = 0; i < 2; ++i) g[i] = *reinterpret_cast<const f32x4 *>(eG + 32 * kb + 16 * i + 4 * q);
             const Split o = operand<Split>(d[2 * kb] * (z.scale * g[0]), d[2 * kb + 1] * (z.scale * g[1]));
-            if (sizeof(E) == 4) fence();
-            const Split r = operand<Split>(R[2 * kb] * (-b[2 * kb] * g[0]), R[2 * kb + 1] * (-b[2 * kb + 1] * g[1]));
 #pragma unroll
-            for (int t = 0; t < DK / 16; ++t) {
-                S[t] = mma(tile8<X, L::kTok>(Qt, 16 * t, 32 * kb, lane), o, S[t]);
-                S[t] = mma(tile8<X, L::kTok>(Kt, 16 * t, 32 * kb, lane), r, S[t]);
-            }
+            for (int t = 0; t < DK / 16; ++t) S[t] = mma(tile8<X, L::kTok>(Qt, 16 * t, 32 * kb, lane), o, S[t]);
+            if (FULL) fence();
+            const Split r = operand<Split>(R[2 * kb] * (-strengths(2 * kb) * g[0]), R[2 * kb + 1] * (-strengths(2 * kb + 1) * g[1]));
+#pragma unroll
+            for (int t = 0; t < DK / 16; ++t) S[t] = mma(tile8<X, L::kTok>(Kt, 16 * t, 32 * kb, lane), r, S[t]);
+            if (FULL) fence();
         }
         if (!kAhead && c > c0) take_columns(c - 1);
     }
@@ -812,47 +804,23 @@ struct GradArgs {
     float *dg, *dbeta;
 };
 
-// what the 32 x 32 products of this kernel take: rows row0 + lane % 32 of a tile in LDS, 16 places from k0
-template <class X, int STRIDE>
-__device__ __forceinline__ typename X::Exact tall8(const typename X::E *t, int row0, int k0, int lane)
-{
-    return get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5));
-}
-template <class OPERAND, int STRIDE, class E>
-__device__ __forceinline__ OPERAND tall8s(const E *t, int row0, int k0, int lane)
-{
-    OPERAND x;
-    get8(t + (row0 + (lane & 31)) * STRIDE + k0 + 8 * (lane >> 5), C * STRIDE, x);
-    return x;
-}
-// an accumulator of 32 tokens, stored row by row, rounded to the element type
+// the elements of a caller's row at eight places of the spread order, from place p (a multiple of 8)
 template <class X>
-__device__ __forceinline__ void store_tall(typename X::E *p, int row0, int rows, int width, int k0, const f32x16 &c, int lane)
+__device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *t, int row, int rows, int width, int p)
 {
-    f32x16 t = zero16();
-#pragma unroll
-    for (int g16 = 0; g16 < 2; ++g16) {
-        float x[8];
-        typename X::Exact s;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = c[8 * g16 + e];
-        round8(x, s);
-        t = mma(s, unit8<X, 32, true>(g16, lane), t);
-    }
-    const int row = row0 + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int k = k0 + 8 * i + 4 * (lane >> 5);
-        const float x[4] = {t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]};
-        if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, x);
-    }
+    const int k = (p & ~31) + ((p & 31) >> 1);
+    return load8_spread(t + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 16 < width);
 }
-
-// sums over the 32 lanes of a half of 32 values a lane: afterwards lane l holds the sum of value sum32_index(l)
-__device__ __forceinline__ float sum32(float (&v)[32], int lane)
+// sums over 16 lanes of 4 TI values a lane: afterwards lane l holds the sum of value l % (4 TI)
+template <int TI>
+__device__ __forceinline__ float sum_lanes(float (&v)[4 * TI], int lane)
 {
 #pragma unroll
-    for (int m = 16; m >= 1; m /= 2) {
+    for (int m = 8; m >= 4 * TI; m /= 2)
+#pragma unroll
+        for (int k = 0; k < 4 * TI; ++k) v[k] += __shfl_xor(v[k], m);
+#pragma unroll
+    for (int m = 2 * TI; m >= 1; m /= 2) {
         const bool up = lane & m;
 #pragma unroll
         for (int k = 0; k < m; ++k) {
@@ -862,27 +830,41 @@ __device__ __forceinline__ float sum32(float (&v)[32], int lane)
     }
     return v[0];
 }
-__device__ __forceinline__ int sum32_index(int lane) { return lane & 31; }
 
-// the elements of a caller's row at eight places of the spread order, from place p (a multiple of 8)
-template <class X>
-__device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *t, int row, int rows, int width, int p)
-{
-    const int k = (p & ~31) + ((p & 31) >> 1);
-    return load8_spread(t + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 16 < width);
-}
+// One workgroup of eight wavefronts per chunk.  U, dR and dO are read once, into LDS, as operands; a wavefront then has 16 columns of dQ and dK
+// (and with dk <= 64 half of the tokens), for which it reads its rows of S and dS once, as right operands: dO S^T, dR S^T and U dS^T.  F and E are
+// formed from the same tiles before these are overwritten with F, F^T and E + E^T, whose products with K and Q end the kernel.
+constexpr int kGradThreads = 512;
 
 template <class X, int DK>
-__global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
-{
+struct GradLds {
     typedef typename X::E E;
     typedef Lds<X, DK> L;
+    static constexpr int kWide = 128 + X::kPad;                         // a token's row over columns of the state, in spread order
+    static constexpr bool kHasO = sizeof(E) == 2;                       // dO has no room beside fp32 tiles: its operands come from memory
+    static constexpr int kFloats = 3 * C + 8 * C + C + 8;               // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
+    static constexpr int kTiles = C * kWide * (X::kPlanes + X::kPairPlanes + (kHasO ? 1 : 0));
+    static constexpr size_t kBytes = C * sizeof(double) + kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
+    static_assert((X::kPlanes + 2 * X::kPairPlanes) * L::kSquare <= kTiles, "F, F^T and E + E^T lie where U, dR and dO were");
+};
+
+template <class X, int DK>
+__global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
+{
+    typedef typename X::E E;
+    typedef typename X::Exact Exact;
+    typedef typename X::Pair Pair;
+    typedef typename X::Split Split;
+    typedef Lds<X, DK> L;
+    typedef GradLds<X, DK> G;
+    constexpr int kWide = G::kWide, kTok = L::kTok, TI = DK / 32;       // TI: 16-token tiles of a wavefront
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    double *G = reinterpret_cast<double *>(lds_raw);
-    float *eG = reinterpret_cast<float *>(G + C), *eEnd = eG + C, *bs = eEnd + C, *qd = bs + C /* 4 C */, *vd = qd + 4 * C, *part = vd + C /* 8 */;
-    E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *F = Qt + L::kByRows, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
+    double *Gs = reinterpret_cast<double *>(lds_raw);
+    float *eG = reinterpret_cast<float *>(Gs + C), *eEnd = eG + C, *bs = eEnd + C, *qd = bs + C, *vd = qd + 8 * C, *part = vd + C;
+    E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPairPlanes * C * kWide;
+    E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, q = lane >> 4, col = lane & 15;
     const int bh = blockIdx.y, c = blockIdx.x, n = tokens_of(z, z.chunk0 + c);
     const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
     const size_t at = static_cast<size_t>(bh) * z.chunks + c;
@@ -890,189 +872,243 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(GradArgs a)
     const E *V = static_cast<const E *>(a.V) + row0 * z.dv, *dO = static_cast<const E *>(a.dO) + row0 * z.dv;
     const float *S = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, *dS = a.dS + at * DK * z.dvp;
     const float *U = a.U + at * C * z.dvp, *dR = a.dR + at * C * z.dvp;
+    const int deep = z.dvp / 32;            // steps of a product over the state's columns
+    const int dcol = 16 * (wave % (DK / 16)) + col, ti0 = wave / (DK / 16) * TI;
 
-    if (wave == 3) {
+    if (wave == 7) {
         const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[row0 + lane])) : 0.0, lane);
-        G[lane] = g;
+        Gs[lane] = g;
         eG[lane] = expf(static_cast<float>(g));
         eEnd[lane] = expf(static_cast<float>(__shfl(g, 63) - g));
         bs[lane] = lane < n ? strength(a.beta[row0 + lane]) : kBetaFloor;
     }
-    qd[tid] = 0.f;
+    for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
     {
-        RowsStage<X, DK> ks, qs;
-        if (tid < 2 * DK) {
-            ks.take(K, n, z.dk, tid);
-            qs.take(Q, n, z.dk, tid);
-            ks.template put<false, true, false>(n, z.dk, nullptr, Kt, tid);
-            qs.template put<false, true, false>(n, z.dk, nullptr, Qt, tid);
+        RowsStage<X, DK> rows;
+        const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
+        const int task = has_k ? tid : tid - (kGradThreads - 2 * DK);
+        if (has_k || has_q) {
+            rows.take(has_k ? K : Q, n, z.dk, task);
+            rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
+        }
+    }
+    // the tiles, and on the way u.dR and v.dR of every token: 16 lanes a row, eight places each
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int i = (tid >> 4) + 32 * half, p = 8 * (tid & 15);
+        float u[8], r[8], v[8], ud = 0.f, vr = 0.f;
+        const bool there = p < z.dvp;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = r[e] = 0.f;
+        if (there) {
+            kept8(U + i * z.dvp + p, u);
+            kept8(dR + i * z.dvp + p, r);
+        }
+        values8(rows8_spread<X>(V, i, there ? n : 0, z.dv, p), v);
+        const Exact o = rows8_spread<X>(dO, i, there ? n : 0, z.dv, p);
+        Split us;
+        Pair rs;
+        split8(u, us);
+        split8(r, rs);
+        put8(Us + i * kWide + p, C * kWide, us);
+        put8(Rs + i * kWide + p, C * kWide, rs);
+        if (G::kHasO) put8(Os + i * kWide + p, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ud += u[e] * r[e];
+            vr += v[e] * r[e];
+        }
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) {
+            ud += __shfl_xor(ud, m);
+            vr += __shfl_xor(vr, m);
+        }
+        if ((tid & 15) == 0) {
+            const float b = i < n ? strength(a.beta[row0 + i]) : kBetaFloor;
+            vd[i] = b * vr;
+            if (i < n) a.dbeta[row0 + i] = ud / b;
         }
     }
     __syncthreads();
+    // rows of the left operands: 16 tokens of a tile, 32 places from p
+    auto tokens_o = [&](int row, int p) -> Exact {
+        if (G::kHasO) return get8(Os + (row + col) * kWide + p + 8 * q);
+        return rows8_spread<X>(dO, row + col, n, z.dv, p + 8 * q);
+    };
 
-    // per token: u.dR and v.dV; over the states <S', dS>
-    {
-        const int i = tid >> 2;
-        float ud = 0.f, vr = 0.f;
-        for (int o = tid & 3; o < z.dvp / 8; o += 4) {
-            float u[8], r[8], v[8];
-            kept8(U + i * z.dvp + 8 * o, u);
-            kept8(dR + i * z.dvp + 8 * o, r);
-            values8(rows8_spread<X>(V, i, n, z.dv, 8 * o), v);
+    // F (jobs 0 .. 9) and E (10 .. 19): 16 x 16 tiles on and below the diagonal; rows j, columns i
+    f32x4 jobs[3];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ud += u[e] * r[e];
-                vr += v[e] * r[e];
+    for (int k = 0; k < 3; ++k) {
+        jobs[k] = zero4();
+        const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
+        if (job >= 20) continue;
+        const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
+#pragma unroll 1
+        for (int kb = 0; kb < deep; ++kb) {
+            const int p = 32 * kb;
+            if (job < 10) {
+                Split u;
+                get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
+                jobs[k] = mma(u, tokens_o(16 * ti, p), jobs[k]);
+            } else {
+                Pair u, r;
+                get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
+                get8(Rs + (16 * ti + col) * kWide + p + 8 * q, C * kWide, r);
+                jobs[k] = mma(u, r, jobs[k]);
             }
         }
-        ud += __shfl_xor(ud, 1);
-        vr += __shfl_xor(vr, 1);
-        ud += __shfl_xor(ud, 2);
-        vr += __shfl_xor(vr, 2);
-        if ((tid & 3) == 0) {
-            vd[i] = bs[i] * vr;
-            if (i < n) a.dbeta[row0 + i] = ud / bs[i];
-        }
-        const float *S1 = S + DK * z.dvp;
-        float dot = 0.f;
-        for (int o = tid; o < DK * z.dvp / 8; o += 256) {
-            float x[8], y[8];
-            kept8(S1 + 8 * o, x);
-            kept8(dS + 8 * o, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot += x[e] * y[e];
-        }
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
-        if (lane == 0) part[wave] = dot;
     }
-    // F, its transpose, and E + E^T
-    if (wave < 3) {
-        const int ti = wave > 0 ? 1 : 0, tj = wave == 2 ? 1 : 0;
-        f32x16 zz = zero16(), xx = zero16();         // rows j, columns i
-        for (int kb = 0; kb < z.dvp / 16; ++kb) {
-            const int k0 = 16 * kb + 8 * h;
-            const typename X::Split uj = kept<typename X::Split>(U + (32 * tj + col) * z.dvp + k0);
-            zz = mma(uj, rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb + 8 * h), zz);
-            xx = mma(lead(uj), kept<typename X::Pair>(dR + (32 * ti + col) * z.dvp + k0), xx);
+    // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T; over the states <S', dS>
+    f32x4 dq[TI], dk[TI], y[TI];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) dq[t] = dk[t] = y[t] = zero4();
+    float dot = 0.f;
+#pragma unroll 1
+    for (int kb = 0; kb < deep; ++kb) {
+        const int p = 32 * kb;
+        float s[8], d[8], s1[8];
+        kept8(S + dcol * z.dvp + p + 8 * q, s);
+        kept8(dS + dcol * z.dvp + p + 8 * q, d);
+        kept8(S + (DK + dcol) * z.dvp + p + 8 * q, s1);
+        Split ss;
+        Pair ds;
+        split8(s, ss);
+        split8(d, ds);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot += s1[e] * d[e];
+#pragma unroll
+        for (int t = 0; t < TI; ++t) {
+            const int row = 16 * (ti0 + t);
+            Pair u, r;
+            get8(Us + (row + col) * kWide + p + 8 * q, C * kWide, u);
+            get8(Rs + (row + col) * kWide + p + 8 * q, C * kWide, r);
+            dq[t] = mma(tokens_o(row, p), ss, dq[t]);
+            y[t] = mma(r, lead(ss), y[t]);
+            dk[t] = mma(u, ds, dk[t]);
         }
-        const int i = 32 * ti + col;
+    }
+    if (ti0 > 0) dot = 0.f;         // with dk <= 64 two wavefronts have met the same rows
 #pragma unroll
-        for (int g16 = 0; g16 < 2; ++g16) {
-            float f[8], e8[8];
+    for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
+    if (lane == 0) part[wave] = dot;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = 32 * tj + acc_row(8 * g16 + e, h);
-                const float D = j <= i ? expf(static_cast<float>(G[i] - G[j])) : 0.f;
-                f[e] = z.scale * D * zz[8 * g16 + e];
-                e8[e] = j < i ? -bs[i] * D * xx[8 * g16 + e] : 0.f;
-                if (j > i) f[e] = 0.f;
-            }
-#pragma unroll
-            for (int i8 = 0; i8 < 2; ++i8) {
-                const int to = 32 * tj + spread(16 * g16 + 8 * i8 + 4 * h);
-                put4(F + i * L::kTok + to, L::kSquare, f32x4{f[4 * i8], f[4 * i8 + 1], f[4 * i8 + 2], f[4 * i8 + 3]});
-                put4_pair(Es + i * L::kTok + to, L::kSquare, f32x4{e8[4 * i8], e8[4 * i8 + 1], e8[4 * i8 + 2], e8[4 * i8 + 3]});
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = 32 * tj + acc_row(8 * g16 + e, h);
-                put1_pair(Ft + j * L::kTok + spread(i), L::kSquare, f[e]);
-            }
-        }
-        // after the rows: in a diagonal tile these places hold its zeros
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = 32 * tj + acc_row(e, h);
-            if (j < i) put1_pair(Es + j * L::kTok + spread(i), L::kSquare, -bs[i] * expf(static_cast<float>(G[i] - G[j])) * xx[e]);
-        }
+    for (int t = 0; t < TI; ++t) {
+        const int i = 16 * (ti0 + t) + 4 * q;
+        const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + i), b = *reinterpret_cast<const f32x4 *>(bs + i);
+        dq[t] *= z.scale * g;
+        dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b * g * y[t];
     }
     __syncthreads();
-    for (int task = wave; task < DK / 16; task += 4) {
-        const bool isq = task < DK / 32;
-        const int d0 = 32 * (isq ? task : task - DK / 32), dcol = d0 + col;
-        f32x16 R[2] = {zero16(), zero16()};
-        if (isq) {
-            for (int kb = 0; kb < z.dvp / 16; ++kb) {
-                const int k0 = 16 * kb + 8 * h;
-                const typename X::Split s = kept<typename X::Split>(S + dcol * z.dvp + k0);
+    // F, its transpose, and E + E^T
 #pragma unroll
-                for (int ti = 0; ti < 2; ++ti) R[ti] = mma(rows8_spread<X>(dO, 32 * ti + col, n, z.dv, 16 * kb + 8 * h), s, R[ti]);
-            }
+    for (int k = 0; k < 3; ++k) {
+        const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
+        if (job >= 20) continue;
+        const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
+        const int i = 16 * ti + col, j0 = 16 * tj + 4 * q;
+        f32x4 D;
 #pragma unroll
-            for (int ti = 0; ti < 2; ++ti)
+        for (int e = 0; e < 4; ++e) D[e] = j0 + e <= i ? expf(static_cast<float>(Gs[i] - Gs[j0 + e])) : 0.f;
+        if (job < 10) {
+            const f32x4 f = z.scale * D * jobs[k];
+            f32x4 f0;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) R[ti][e] *= z.scale * eG[32 * ti + acc_row(e, h)];
+            for (int e = 0; e < 4; ++e) f0[e] = j0 + e <= i ? f[e] : 0.f;
+            put4(F + i * kTok + spread(j0), L::kSquare, f0);
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                const typename X::Exact k = tall8<X, L::kTok>(Kt, d0, 16 * kb, lane);
-#pragma unroll
-                for (int ti = kb >> 1; ti < 2; ++ti) R[ti] = mma(tall8s<typename X::Split, L::kTok>(F, 32 * ti, 16 * kb, lane), k, R[ti]);
-            }
-            float p[32];
-#pragma unroll
-            for (int ti = 0; ti < 2; ++ti)
-#pragma unroll
-                for (int g16 = 0; g16 < 2; ++g16)
-#pragma unroll
-                    for (int i8 = 0; i8 < 2; ++i8) {
-                        float q[4];
-                        get4(Qt + dcol * L::kTok + 32 * ti + spread(16 * g16 + 8 * i8 + 4 * h), q);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) p[16 * ti + 8 * g16 + 4 * i8 + e] = q[e] * R[ti][8 * g16 + 4 * i8 + e];
-                    }
-            const float s = sum32(p, lane);
-            const int v = sum32_index(lane);
-            qd[wave * C + 32 * (v >> 4) + acc_row(v & 15, h)] += s;
+            for (int e = 0; e < 4; ++e) put1_pair(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
         } else {
-            f32x16 Y[2] = {zero16(), zero16()};
-            for (int kb = 0; kb < z.dvp / 16; ++kb) {
-                const int k0 = 16 * kb + 8 * h;
-                const typename X::Pair ds = kept<typename X::Pair>(dS + dcol * z.dvp + k0), s = kept<typename X::Pair>(S + dcol * z.dvp + k0);
+            const f32x4 x = -bs[i] * D * jobs[k];
+            f32x4 x0;
 #pragma unroll
-                for (int ti = 0; ti < 2; ++ti) {
-                    R[ti] = mma(kept<typename X::Pair>(U + (32 * ti + col) * z.dvp + k0), ds, R[ti]);
-                    Y[ti] = mma(kept<typename X::Pair>(dR + (32 * ti + col) * z.dvp + k0), s, Y[ti]);
-                }
+            for (int e = 0; e < 4; ++e) x0[e] = j0 + e < i ? x[e] : 0.f;
+            put4_pair(Es + i * kTok + spread(j0), L::kSquare, x0);
+            // after the rows: in a diagonal tile these places hold its zeros
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, x[e]);
+        }
+    }
+    // what F and F^T have not: half of the steps of 32 tokens on the diagonal
+    if (wave >= 4) {
+        const int t = 2 * (wave & 1);
+        E *to = wave < 6 ? F + (16 * t + col) * kTok + spread(16 * t + 16 + 4 * q) : Ft + (16 * t + 16 + col) * kTok + spread(16 * t + 4 * q);
+        if (wave < 6) put4(to, L::kSquare, zero4());
+        else put4_pair(to, L::kSquare, zero4());
+    }
+    __syncthreads();
+    // dQ += F K, dK += F^T Q + (E + E^T) K
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const int p = 32 * kb + 8 * q;
+        const Exact k = get8(Kt + dcol * kTok + p), qq = get8(Qt + dcol * kTok + p);
+#pragma unroll
+        for (int t = 0; t < TI; ++t) {
+            const int ti = ti0 + t;
+            Pair e;
+            get8(Es + (16 * ti + col) * kTok + p, L::kSquare, e);
+            dk[t] = mma(e, k, dk[t]);
+            if (ti >= 2 * kb) {         // F is lower triangular
+                Split f;
+                get8(F + (16 * ti + col) * kTok + p, L::kSquare, f);
+                dq[t] = mma(f, k, dq[t]);
             }
-#pragma unroll
-            for (int ti = 0; ti < 2; ++ti)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int i = 32 * ti + acc_row(e, h);
-                    R[ti][e] = eEnd[i] * R[ti][e] - bs[i] * eG[i] * Y[ti][e];
-                }
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                const typename X::Exact k = tall8<X, L::kTok>(Kt, d0, 16 * kb, lane), q = tall8<X, L::kTok>(Qt, d0, 16 * kb, lane);
-#pragma unroll
-                for (int ti = 0; ti < 2; ++ti) {
-                    R[ti] = mma(tall8s<typename X::Pair, L::kTok>(Es, 32 * ti, 16 * kb, lane), k, R[ti]);
-                    if (ti <= kb >> 1) R[ti] = mma(tall8s<typename X::Pair, L::kTok>(Ft, 32 * ti, 16 * kb, lane), q, R[ti]);
-                }
+            if (ti < 2 * kb + 2) {
+                Pair f;
+                get8(Ft + (16 * ti + col) * kTok + p, L::kSquare, f);
+                dk[t] = mma(f, qq, dk[t]);
             }
         }
+    }
+    {
+        float v[4 * TI];
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) {
-            if (!a.shared) {
-                store_tall<X>(static_cast<E *>(isq ? a.dQ : a.dK) + qk_row(z, bh, t0) * z.dk, 32 * ti, n, z.dk, d0, R[ti], lane);
-                continue;
+        for (int t = 0; t < TI; ++t) {
+            float x[4];
+            get4(Qt + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * dq[t][e];
+        }
+        const float s = sum_lanes<TI>(v, lane);
+        const int w = col % (4 * TI);
+        if (col < 4 * TI) qd[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
+    }
+    const int d0 = dcol - col;
+    if (a.shared) {
+        const buffer_t outq = buffer(static_cast<float *>(a.dQ) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+        const buffer_t outk = buffer(static_cast<float *>(a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+#pragma unroll
+        for (int t = 0; t < TI; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int to = state_offset(16 * (ti0 + t) + 4 * q + e, z.dk, dcol);
+                put_buffer(outq, to, dq[t][e]);
+                put_buffer(outk, to, dk[t][e]);
             }
-            const buffer_t out = buffer(static_cast<float *>(isq ? a.dQ : a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+    } else {
+        E *outq = static_cast<E *>(a.dQ) + qk_row(z, bh, t0) * z.dk, *outk = static_cast<E *>(a.dK) + qk_row(z, bh, t0) * z.dk;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) put_buffer(out, state_offset(32 * ti + acc_row(e, h), z.dk, dcol), R[ti][e]);
+        for (int t = 0; t < TI; t += 2) {
+            store_rows<X>(outq, 16 * (ti0 + t), n, z.dk, d0, dq[t], dq[t + 1], lane);
+            store_rows<X>(outk, 16 * (ti0 + t), n, z.dk, d0, dk[t], dk[t + 1], lane);
         }
     }
     __syncthreads();
     if (wave == 0) {
-        const float mine = qd[lane] + qd[C + lane] + qd[2 * C + lane] + qd[3 * C + lane] - vd[lane];
+        float mine = -vd[lane], tail = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            mine += qd[w * C + lane];
+            tail += part[w];
+        }
         float s = mine;         // sum over this token and those behind it
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const float y = __shfl_down(s, d);
             if (lane + d < 64) s += y;
         }
-        if (lane < n) a.dg[row0 + lane] = s + (part[0] + part[1] + part[2] + part[3]);
+        if (lane < n) a.dg[row0 + lane] = s + tail;
     }
 }
 
@@ -1167,13 +1203,6 @@ constexpr size_t rev_lds()
     typedef Lds<X, DK> L;
     return sizeof(typename X::E) * (L::kByTokens + 2 * L::kByRows + 2 * X::kPlanes * L::kSquare) + 3 * C * sizeof(float);
 }
-template <class X, int DK>
-constexpr size_t grad_lds()
-{
-    typedef Lds<X, DK> L;
-    return sizeof(typename X::E) * (2 * L::kByRows + (X::kPlanes + 2 * X::kPairPlanes) * L::kSquare) + C * sizeof(double) + (8 * C + 8) * sizeof(float);
-}
-
 float *floats(char *ws, size_t at) { return reinterpret_cast<float *>(ws + at); }
 
 Sizes sizes_of(const DeltaPlan &p)
@@ -1369,7 +1398,7 @@ struct Passes {
             const bool shared = p.H != p.Hk;
             GradArgs g{z, io.Q, io.K, io.V, io.dO, io.g, io.beta, a_S, a_U, full.dS, full.dR,
                        shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta};
-            DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3(z.chunks, p.BH), 256, (grad_lds<X, DK>()), st, g);
+            DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3(z.chunks, p.BH), kGradThreads, (GradLds<X, DK>::kBytes), st, g);
             if (shared) {
                 const int rows = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(z.chunks) * C, p.N - static_cast<int64_t>(z.chunk0) * C));
                 const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(rows) * p.dk + 255) / 256), p.BH / p.H * p.Hk);
