@@ -584,8 +584,8 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 
 // ------------------------------------------------------------------ states at the segments' starts
 // S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 columns, a
-// wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and the next step's P
-// and B are in registers before the present one's products begin.
+// wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
+// asked for two steps ahead.
 struct CombineArgs {
     Sizes z;
     const float *carry;             // state to start from (null: zero): carry + bh * carry_head
@@ -594,6 +594,7 @@ struct CombineArgs {
     const float *add;               // B_s: add + (bh * nseg + s) * dk * dv
     float *at;                      // states at the segments' starts (REV: cotangents at their ends), same layout, nseg + 1 (REV: nseg) of them a head
     size_t at_head;
+    int heads;
     int steps;                      // transitions taken: segments seg0 .. seg0 + steps - 1 (REV: seg0 + segs - 1 down)
 };
 
@@ -604,41 +605,48 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     typedef typename X::Split Split;
     __shared__ __attribute__((aligned(16))) E ops[2][X::kPlanes][DK / 32][64 * 8];
     const Sizes &z = a.z;
-    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * blockIdx.x + (lane & 15), bh = blockIdx.y;
+    // workgroups go to the eight XCDs in turn: those of one head to the same one, whose L2 then fetches P once
+    const int tiles = z.dvp / 16, slot = blockIdx.x >> 3, bh = slot / tiles * 8 + (blockIdx.x & 7);
+    if (bh >= a.heads) return;
+    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * (slot % tiles) + (lane & 15);
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
     auto segment = [&](int i) { return REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i; };
-    Split P[DK / 32];
-    f32x4 B[1], S[1] = {zero4()};
-    auto take = [&](int i) {
+    struct Step {
+        Split P[DK / 32];
+        f32x4 B[1];
+    } ahead[2];
+    f32x4 S[1] = {zero4()};
+    auto take = [&](int i, Step &to) {
         const size_t s = static_cast<size_t>(bh) * z.nseg + segment(i);
         const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + state_row(wave, lane >> 2 & 3, lane & 3) * DK + 8 * q;
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, P[kb]);
-        get_state(B, a.add + s * one, z.dk, z.dv, wave, col, lane);
+        for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, to.P[kb]);
+        get_state(to.B, a.add + s * one, z.dk, z.dv, wave, col, lane);
     };
-    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, wave, col, lane);
-    if (a.steps > 0) take(0);
-    for (int i = 0; i <= a.steps; ++i) {
-        put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane);
-        if (i == a.steps) break;
+    auto put = [&](int i) { put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane); };
+    auto step = [&](int i, Step &my, E (*op)[DK / 32][64 * 8]) {
+        put(i);
         // the lane's four rows are half of its eight places in the operand of 32 rows
-        put4(&ops[i & 1][0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[0]);
-        Split p[DK / 32];
-#pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) p[kb] = P[kb];
-        S[0] = B[0];
-        f32x4 more = zero4();
+        put4(&op[0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[0]);
+        f32x4 sums[2] = {my.B[0], zero4()};
         __syncthreads();
-        if (i + 1 < a.steps) take(i + 1);
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
             Split s;
-            get8(&ops[i & 1][0][kb][lane * 8], DK / 32 * 64 * 8, s);
-            if (kb & 1) more = mma(p[kb], s, more);
-            else S[0] = mma(p[kb], s, S[0]);
+            get8(&op[0][kb][lane * 8], DK / 32 * 64 * 8, s);
+            sums[kb & 1] = mma(my.P[kb], s, sums[kb & 1]);
         }
-        S[0] += more;
+        S[0] = sums[0] + sums[1];
+        if (i + 2 < a.steps) take(i + 2, my);
+    };
+    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, wave, col, lane);
+    if (a.steps > 0) take(0, ahead[0]);
+    if (a.steps > 1) take(1, ahead[1]);
+    for (int i = 0; i < a.steps; i += 2) {
+        step(i, ahead[0], ops[0]);
+        if (i + 1 < a.steps) step(i + 1, ahead[1], ops[1]);
     }
+    put(a.steps);
 }
 
 // ------------------------------------------------------------------ cotangents of the states, last chunk first
@@ -1283,8 +1291,9 @@ struct Passes {
         a.add = floats(ws, p.off_add);
         a.at = floats(ws, rev ? p.off_end : p.off_start);
         a.at_head = static_cast<size_t>(p.dk) * p.dv * (rev ? p.nseg : p.nseg + 1);
+        a.heads = p.BH;
         a.steps = steps;
-        const dim3 grid(p.dvp / 16, p.BH);
+        const int grid = (p.BH + 7) / 8 * 8 * (p.dvp / 16);
         if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 4 * DK, 0, st, a);
         else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 4 * DK, 0, st, a);
         return hipSuccess;

@@ -24,8 +24,8 @@ race_status_t check_workspace(const void *ws, size_t bytes, size_t need)
 }
 
 // ---------------------------------------------------------------- gated delta rule
-// Chunks of a head that a window holds: its share of kWindowChunks, which bounds the workspace.
-constexpr int kWindowChunks = 16384;
+// What a window's chunks may take of the workspace.
+constexpr size_t kWindowBytes = size_t(4) << 30;
 
 race_status_t check_delta(const race_delta_desc_t *d)
 {
@@ -74,7 +74,9 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         *pl = p;
         return RACE_OK;
     }
-    const int window = std::max(1, std::min(p.chunks, kWindowChunks / p.BH));
+    const size_t dkp = d->dk <= 64 ? 64 : 128, split = d->dtype == RACE_F32 ? 4 : 6, one = sizeof(float) * p.dk * p.dv, square = kChunk * kChunk;
+    const size_t per_chunk = square * 8 + 3 * kChunk * 4 + (backward ? square * 4 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
+    const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
         p.seg_chunks = static_cast<int>(std::min<int64_t>((d->chunk + kChunk - 1) / kChunk, p.chunks));
         p.win_segs = std::max(1, window / p.seg_chunks);
@@ -86,8 +88,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     p.win_segs = std::min({p.win_segs, p.nseg, 65535});
     p.windows = (p.nseg + p.win_segs - 1) / p.win_segs;
 
-    const size_t dkp = d->dk <= 64 ? 64 : 128, split = d->dtype == RACE_F32 ? 4 : 6, one = sizeof(float) * p.dk * p.dv;
-    const size_t n = static_cast<size_t>(p.BH) * std::min<int64_t>(static_cast<int64_t>(p.win_segs) * p.seg_chunks, p.chunks), square = kChunk * kChunk;
+    const size_t n = static_cast<size_t>(p.BH) * std::min<int64_t>(static_cast<int64_t>(p.win_segs) * p.seg_chunks, p.chunks);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;

@@ -115,17 +115,48 @@ def test_keys_alike(dtype):
     _check(_got(x), _want(x), dtype, "alike")
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("B,H,Hk,N,dk,chunk", [(64, 128, 64, 150, 8, 0), (1, 128, 64, 64 * 140 - 7, 8, 0)])
-def test_more_than_one_window(B, H, Hk, N, dk, chunk, dtype):
-    """So many heads, or so many tokens of many heads, that the workspace is used for one part of the sequence after another."""
-    x = _inputs(B, H, Hk, N, dk, dk, dtype, seed=1)
-    d = _desc(x, chunk)
-    whole = B * H * -(-N // 64)
-    assert whole > 16384
-    _check(_got(x, chunk), _want(x), dtype, "windows")
-    # the workspace is not that of the whole sequence
-    assert ra.race_delta_bwd_workspace_bytes(d) < 4 * whole * (64 * 64 + 64 * 64)* 4
+def test_more_than_one_window():
+    """So many heads that the backward pass uses its workspace for one part of the sequence after another."""
+    B, H, Hk, N, dk = 64, 128, 64, 450, 8
+    x = _inputs(B, H, Hk, N, dk, dk, "bf16", seed=1)
+    assert ra.race_delta_segment_tokens(_desc(x)) == 512 and _windows(_desc(x)) > 1
+    _check(_got(x), _want(x), "bf16", "windows")
+
+
+def _windows(d):
+    """Whether a sequence twice as long takes less than twice the workspace: the backward pass goes by windows."""
+    twice = ra.make_delta_desc(d.B, d.H, d.Hk, 2 * d.N, d.dk, d.dv, d.scale, d.dtype, d.chunk)
+    return 2 if ra.race_delta_bwd_workspace_bytes(twice) < 1.5 * ra.race_delta_bwd_workspace_bytes(d) else 1
+
+
+@pytest.mark.parametrize("B,H,N,cut", [(1, 128, 64 * 420 - 7, 64 * 200), (255, 257, 64 * 5, 64 * 2)])
+def test_windows_against_parts(B, H, N, cut):
+    """Windows of several segments each, and windows of the forward pass: the sequence in one call against its two parts, the state and its cotangent carried."""
+    dk = 8
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    t = torch.bfloat16
+    Q, K = (torch.nn.functional.normalize(torch.randn((B, H, N, dk), generator=gen, device="cuda"), dim=-1).to(t) for _ in range(2))
+    V, dO = (torch.randn((B, H, N, dk), generator=gen, device="cuda").to(t) for _ in range(2))
+    g, beta = -0.05 * torch.rand((B, H, N), generator=gen, device="cuda"), torch.rand((B, H, N), generator=gen, device="cuda")
+    S, dS = (torch.randn((B, H, dk, dk), generator=gen, device="cuda") for _ in range(2))
+    desc = lambda n: ra.make_delta_desc(B, H, H, n, dk, dk, 0.3, ra.RACE_BF16)  # noqa: E731
+    assert _windows(desc(N)) == 2
+    x = (Q, K, V, g, beta)
+    O, end = ra.race_delta_fwd(desc(N), *x, state_in=S, want_state=True)
+    grads = ra.race_delta_bwd(desc(N), *x, dO, state_in=S, dstate_out=dS, want_dstate=True)
+    head, tail = ([v[:, :, sl].contiguous() for v in x + (dO,)] for sl in (slice(0, cut), slice(cut, N)))
+    Oh, mid = ra.race_delta_fwd(desc(cut), *head[:5], state_in=S, want_state=True)
+    Ot, out = ra.race_delta_fwd(desc(N - cut), *tail[:5], state_in=mid, want_state=True)
+    gt = ra.race_delta_bwd(desc(N - cut), *tail, state_in=mid, dstate_out=dS, want_dstate=True)
+    gh = ra.race_delta_bwd(desc(cut), *head, state_in=S, dstate_out=gt[5], want_dstate=True)
+    names = ("dQ", "dK", "dV", "dg", "dbeta")
+    got = dict({"O": O, "state": end, "dstate": grads[5]}, **dict(zip(names, grads)))
+    want = dict({"O": torch.cat((Oh, Ot), 2), "state": out, "dstate": gh[5]}, **{n: torch.cat((a, b), 2) for n, a, b in zip(names, gh, gt)})
+    for n in want:      # both sides are off by what the tolerances say
+        a, b = got[n].double(), want[n].double()
+        off = ((a - b).norm() / b.norm()).item()
+        print("%s %.2e" % (n, off), flush=True)
+        assert off <= 2 * BF16[n], n
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
