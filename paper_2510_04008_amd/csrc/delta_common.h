@@ -226,6 +226,14 @@ __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(stat
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ void put1(uint16_t *p, float x) { *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
 __device__ __forceinline__ void put1(float *p, float x) { *p = x; }
+__device__ __forceinline__ void put1(uint16_t *p, int plane, float x)
+{
+    const uint32_t hi = round2(x, 0.f), mid = round2(x - low2(hi), 0.f);
+    p[0] = static_cast<uint16_t>(hi);
+    p[plane] = static_cast<uint16_t>(mid);
+    p[2 * plane] = static_cast<uint16_t>(round2(x - low2(hi) - low2(mid), 0.f));
+}
+__device__ __forceinline__ void put1(float *p, int, float x) { *p = x; }
 __device__ __forceinline__ void put1_pair(uint16_t *p, int plane, float x)
 {
     const __bf16 hi = static_cast<__bf16>(x);

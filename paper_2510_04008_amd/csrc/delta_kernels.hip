@@ -585,17 +585,23 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 // ------------------------------------------------------------------ states at the segments' starts
 // S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 columns, a
 // wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
-// asked for two steps ahead.
+// asked for two steps ahead.  A step takes 2 to 3 us all the same, most of it P on its way, so many segments are joined in groups of about the root of
+// their number: the transitions of the groups side by side (compose), the groups one after the other, then the segments of all groups side by side.
 struct CombineArgs {
     Sizes z;
-    const float *carry;             // state to start from (null: zero): carry + bh * carry_head
-    size_t carry_head;
-    const void *P;
-    const float *add;               // B_s: add + (bh * nseg + s) * dk * dv
-    float *at;                      // states at the segments' starts (REV: cotangents at their ends), same layout, nseg + 1 (REV: nseg) of them a head
+    int heads, groups, each;        // transitions of a group: each; the last group's may be fewer
+    int steps;                      // transitions in all: segments first, first + 1, .. (REV: first, first - 1, ..)
+    int first;
+    const void *P;                  // P_s: image bh * p_head + s; B_s: add + (bh * p_head + s) * dk * dv
+    size_t p_head;
+    const float *add;
+    const float *carry;             // state to start from (null: zero): carry + bh * carry_head + group * carry_group
+    size_t carry_head, carry_group;
+    float *at;                      // states at the segments' starts (REV: cotangents at their ends): at + bh * at_head + s * dk * dv; null: not wanted
     size_t at_head;
-    int heads;
-    int steps;                      // transitions taken: segments seg0 .. seg0 + steps - 1 (REV: seg0 + segs - 1 down)
+    void *out_P;                    // compose: the groups' transitions and states from zero, image bh * out_head + group
+    float *out_add;
+    size_t out_head;
 };
 
 template <class X, int DK, bool REV>
@@ -605,25 +611,31 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     typedef typename X::Split Split;
     __shared__ __attribute__((aligned(16))) E ops[2][X::kPlanes][DK / 32][64 * 8];
     const Sizes &z = a.z;
-    // workgroups go to the eight XCDs in turn: those of one head to the same one, whose L2 then fetches P once
-    const int tiles = z.dvp / 16, slot = blockIdx.x >> 3, bh = slot / tiles * 8 + (blockIdx.x & 7);
-    if (bh >= a.heads) return;
-    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * (slot % tiles) + (lane & 15);
+    // workgroups go to the eight XCDs in turn: those of one head and group to the same one, whose L2 then fetches P once
+    const int vtiles = z.dvp / 16, tiles = vtiles + (a.out_P ? DK / 16 : 0), slot = blockIdx.x >> 3, unit = slot / tiles * 8 + (blockIdx.x & 7);
+    if (unit >= a.heads * a.groups) return;
+    const int bh = unit / a.groups, group = unit - bh * a.groups, tile = slot % tiles;
+    const int begin = group * a.each, end = min(begin + a.each, a.steps);
+    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * tile + (lane & 15);
+    const bool trans = tile >= vtiles;
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
-    auto segment = [&](int i) { return REV ? z.seg0 + z.segs - 1 - i : z.seg0 + i; };
+    auto segment = [&](int i) { return REV ? a.first - i : a.first + i; };
     struct Step {
         Split P[DK / 32];
         f32x4 B[1];
     } ahead[2];
     f32x4 S[1] = {zero4()};
     auto take = [&](int i, Step &to) {
-        const size_t s = static_cast<size_t>(bh) * z.nseg + segment(i);
+        const size_t s = static_cast<size_t>(bh) * a.p_head + segment(i);
         const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + state_row(wave, lane >> 2 & 3, lane & 3) * DK + 8 * q;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, to.P[kb]);
-        get_state(to.B, a.add + s * one, z.dk, z.dv, wave, col, lane);
+        to.B[0] = zero4();
+        if (!trans) get_state(to.B, a.add + s * one, z.dk, z.dv, wave, col, lane);
     };
-    auto put = [&](int i) { put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane); };
+    auto put = [&](int i) {
+        if (a.at) put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane);
+    };
     auto step = [&](int i, Step &my, E (*op)[DK / 32][64 * 8]) {
         put(i);
         // the lane's four rows are half of its eight places in the operand of 32 rows
@@ -637,16 +649,32 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
             sums[kb & 1] = mma(my.P[kb], s, sums[kb & 1]);
         }
         S[0] = sums[0] + sums[1];
-        if (i + 2 < a.steps) take(i + 2, my);
+        if (i + 2 < end) take(i + 2, my);
     };
-    if (a.carry) get_state(S, a.carry + bh * a.carry_head, z.dk, z.dv, wave, col, lane);
-    if (a.steps > 0) take(0, ahead[0]);
-    if (a.steps > 1) take(1, ahead[1]);
-    for (int i = 0; i < a.steps; i += 2) {
-        step(i, ahead[0], ops[0]);
-        if (i + 1 < a.steps) step(i + 1, ahead[1], ops[1]);
+    if (trans) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[0][e] = state_row(wave, q, e) == col - z.dvp ? 1.f : 0.f;
+    } else if (a.carry) {
+        get_state(S, a.carry + bh * a.carry_head + group * a.carry_group, z.dk, z.dv, wave, col, lane);
     }
-    put(a.steps);
+    if (begin < end) take(begin, ahead[0]);
+    if (begin + 1 < end) take(begin + 1, ahead[1]);
+    for (int i = begin; i < end; i += 2) {
+        step(i, ahead[0], ops[0]);
+        if (i + 1 < end) step(i + 1, ahead[1], ops[1]);
+    }
+    if (a.out_P) {
+        const size_t g = static_cast<size_t>(bh) * a.out_head + group;
+        if (trans) {
+            E *P = static_cast<E *>(a.out_P) + g * X::kPlanes * DK * DK;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put1(P + state_row(wave, q, e) * DK + col - z.dvp, DK * DK, S[0][e]);
+        } else {
+            put_state(S, a.out_add + g * one, z.dk, z.dv, wave, col, lane);
+        }
+    } else if (group == a.groups - 1) {
+        put(a.steps);
+    }
 }
 
 // ------------------------------------------------------------------ cotangents of the states, last chunk first
@@ -1281,19 +1309,55 @@ struct Passes {
         DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, THREADS, kPre>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
         return hipSuccess;
     }
+    // states at the starts of the window's segments (rev: cotangents at their ends), `steps` transitions from the first (last) on
     static hipError_t combine(const DeltaPlan &p, const Sizes &z, const float *carry, size_t carry_head, char *ws, int steps, bool rev, hipStream_t st)
     {
+        const size_t one = static_cast<size_t>(p.dk) * p.dv;
         CombineArgs a{};
         a.z = z;
+        a.heads = p.BH;
+        a.groups = 1;
+        a.each = a.steps = steps;
+        a.first = rev ? z.seg0 + z.segs - 1 : z.seg0;
+        a.P = ws + (rev ? p.off_PT : p.off_P);
+        a.p_head = p.nseg;
+        a.add = floats(ws, p.off_add);
         a.carry = carry;
         a.carry_head = carry_head;
-        a.P = ws + (rev ? p.off_PT : p.off_P);
-        a.add = floats(ws, p.off_add);
         a.at = floats(ws, rev ? p.off_end : p.off_start);
-        a.at_head = static_cast<size_t>(p.dk) * p.dv * (rev ? p.nseg : p.nseg + 1);
-        a.heads = p.BH;
-        a.steps = steps;
-        const int grid = (p.BH + 7) / 8 * 8 * (p.dvp / 16);
+        a.at_head = one * (rev ? p.nseg : p.nseg + 1);
+        if (p.join_groups > 1 && steps >= kJoinInGroups) {
+            const int each = (steps + p.join_groups - 1) / p.join_groups, groups = (steps + each - 1) / each;
+            // the groups' transitions; the last group's is nobody's
+            CombineArgs c = a;
+            c.groups = groups;
+            c.each = each;
+            c.carry = nullptr;
+            c.at = nullptr;
+            c.out_P = ws + p.off_group_P;
+            c.out_add = floats(ws, p.off_group_add);
+            c.out_head = p.join_groups;
+            if (hipError_t e = launch_combine(c, rev, st); e != hipSuccess) return e;
+            CombineArgs g = a;
+            g.steps = g.each = groups - 1;
+            g.first = 0;
+            g.P = c.out_P;
+            g.p_head = p.join_groups;
+            g.add = c.out_add;
+            g.at = floats(ws, p.off_group_start);
+            g.at_head = one * p.join_groups;
+            if (hipError_t e = launch_combine(g, false, st); e != hipSuccess) return e;
+            a.groups = groups;
+            a.each = each;
+            a.carry = g.at;
+            a.carry_head = g.at_head;
+            a.carry_group = one;
+        }
+        return launch_combine(a, rev, st);
+    }
+    static hipError_t launch_combine(const CombineArgs &a, bool rev, hipStream_t st)
+    {
+        const int tiles = a.z.dvp / 16 + (a.out_P ? DK / 16 : 0), grid = (a.heads * a.groups + 7) / 8 * 8 * tiles;
         if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 4 * DK, 0, st, a);
         else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 4 * DK, 0, st, a);
         return hipSuccess;

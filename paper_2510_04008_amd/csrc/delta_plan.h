@@ -8,6 +8,9 @@
 namespace race {
 namespace delta {
 
+// Fewer transitions than these are joined one after the other: three launches of the root of their number of steps each take no less.
+constexpr int kJoinInGroups = 12;
+
 struct DeltaPlan {
     int B, H, Hk, BH, dk, dv, dvp, dtype;       // dvp: dv rounded up to 32
     int64_t N;
@@ -19,6 +22,8 @@ struct DeltaPlan {
     size_t off_T, off_M, off_dec, off_TT, off_S, off_U, off_dS, off_dR, off_pq, off_pk;
     // per segment of the sequence: states (cotangents) from zero, transitions, states at the starts, cotangents at the ends
     size_t off_add, off_P, off_PT, off_start, off_end;
+    int join_groups;                // at most, of a window's segments (delta_combine_kernel); their transitions, states from zero and starts
+    size_t off_group_P, off_group_add, off_group_start;
     size_t off_carry;               // one state a head between windows
     size_t total;
 };

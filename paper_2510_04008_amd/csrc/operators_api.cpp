@@ -11,6 +11,8 @@
 namespace race {
 namespace {
 
+using delta::kJoinInGroups;
+
 constexpr int kChunk = 64;
 constexpr int kMaxHeads = 65535;            // B H: a grid dimension
 constexpr int64_t kMaxTokens = int64_t(1) << 36;
@@ -79,7 +81,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
         p.seg_chunks = static_cast<int>(std::min<int64_t>((d->chunk + kChunk - 1) / kChunk, p.chunks));
-        p.win_segs = std::max(1, window / p.seg_chunks);
+        p.win_segs = std::max(1, window < p.chunks ? window / p.seg_chunks : (p.chunks + p.seg_chunks - 1) / p.seg_chunks);
     } else {
         p.win_segs = choose_segments(window, p.BH);
         p.seg_chunks = (window + p.win_segs - 1) / p.win_segs;
@@ -103,6 +105,12 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         p.off_add = take(segs * one);
         p.off_P = take(segs * dkp * dkp * split);
         p.off_PT = take(segs * dkp * dkp * split);
+    }
+    if (p.win_segs > kJoinInGroups) {
+        p.join_groups = static_cast<int>(std::lround(std::sqrt(static_cast<double>(p.win_segs))));
+        p.off_group_P = take(static_cast<size_t>(p.BH) * p.join_groups * dkp * dkp * split);
+        p.off_group_add = take(static_cast<size_t>(p.BH) * p.join_groups * one);
+        p.off_group_start = take(static_cast<size_t>(p.BH) * p.join_groups * one);
     }
     if (p.nseg > 1) p.off_start = take((segs + p.BH) * one);
     if (p.windows > 1) p.off_carry = take(p.BH * one);
