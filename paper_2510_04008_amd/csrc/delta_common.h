@@ -40,6 +40,7 @@ typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any2;
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any4;
 
 constexpr int C = 64;               // tokens per chunk
+constexpr int kDec = 5 * C;         // decays and strengths of a chunk
 constexpr float kBetaFloor = 1e-18f;
 constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 0 either way, and -infinity would make differences NaN
 
@@ -208,6 +209,8 @@ __device__ __forceinline__ void put4_pair(uint16_t *p, int plane, const f32x4 &x
 }
 __device__ __forceinline__ void put4(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
 __device__ __forceinline__ void put4_pair(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
+__device__ __forceinline__ void put4_zero(uint16_t *p) { *reinterpret_cast<u32x2 *>(p) = u32x2{0, 0}; }
+__device__ __forceinline__ void put4_zero(float *p) { *reinterpret_cast<f32x4 *>(p) = zero4(); }
 __device__ __forceinline__ void get4(const uint16_t *p, float *x)
 {
     const u32x2 w = *reinterpret_cast<const u32x2 *>(p);

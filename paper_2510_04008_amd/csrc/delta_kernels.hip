@@ -53,44 +53,52 @@ __device__ __forceinline__ OPERAND kept(const float *p)
 }
 
 // ------------------------------------------------------------------ what a chunk needs besides the states
-// T, M and the decays of one chunk of one head.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane per
-// column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions.  Substitution and not powers of A: with keys alike the powers
-// reach thousands where T stays near one.
+// T and the decays of one chunk of one head, and for the backward pass M^T.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane
+// per column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions, each block in A's place.  Substitution and not powers of A: with keys
+// alike the powers reach thousands where T stays near one.
 // Images are written in the order in which the scans' operands lie in LDS (rows in spread order).
 template <int SIZE>
-__device__ __forceinline__ void merge_blocks(float (*A)[68], float (*T)[68], int base, int slab, int lane)
-{
-    const int r16 = lane & 15, q = lane >> 4;
-    constexpr int NT = SIZE / 16;
-    f32x4 P[NT];
+struct MergeBlocks {
+    static constexpr int NT = SIZE / 16;
+    f32x4 R[NT];
+    // -T2 A21 T1 for 16 columns of the pair of blocks that begins at row `base`
+    __device__ __forceinline__ void form(float (*A)[68], int base, int slab, int lane)
+    {
+        const int r16 = lane & 15, q = lane >> 4;
+        f32x4 P[NT];
 #pragma unroll
-    for (int ti = 0; ti < NT; ++ti) {
-        P[ti] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int ti = 0; ti < NT; ++ti) {
+            P[ti] = zero4();
 #pragma unroll
-        for (int k = 0; k < SIZE / 4; ++k)
-            P[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[base + SIZE + 16 * ti + r16][base + 4 * k + q], T[base + 4 * k + q][base + 16 * slab + r16],
-                                                         P[ti], 0, 0, 0);
+            for (int k = 0; k < SIZE / 4; ++k)
+                P[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[base + SIZE + 16 * ti + r16][base + 4 * k + q], A[base + 4 * k + q][base + 16 * slab + r16], P[ti], 0, 0, 0);
+        }
+#pragma unroll
+        for (int ti = 0; ti < NT; ++ti) {
+            R[ti] = zero4();
+#pragma unroll
+            for (int tk = 0; tk < NT; ++tk)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    R[ti] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[base + SIZE + 16 * ti + r16][base + SIZE + 16 * tk + 4 * q + r], P[tk][r], R[ti], 0, 0, 0);
+        }
     }
+    __device__ __forceinline__ void put(float (*A)[68], int base, int slab, int lane) const
+    {
 #pragma unroll
-    for (int ti = 0; ti < NT; ++ti) {
-        f32x4 R = {0.f, 0.f, 0.f, 0.f};
+        for (int ti = 0; ti < NT; ++ti)
 #pragma unroll
-        for (int tk = 0; tk < NT; ++tk)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                R = __builtin_amdgcn_mfma_f32_16x16x4f32(T[base + SIZE + 16 * ti + r16][base + SIZE + 16 * tk + 4 * q + r], P[tk][r], R, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) T[base + SIZE + 16 * ti + 4 * q + r][base + 16 * slab + r16] = -R[r];
+            for (int r = 0; r < 4; ++r) A[base + SIZE + 16 * ti + 4 * (lane >> 4) + r][base + 16 * slab + (lane & 15)] = -R[ti][r];
     }
-}
+};
 
 struct PrepArgs {
     Sizes z;
     const void *Q, *K;
     const float *g, *beta;
-    void *T, *M;            // 64 x 64 images, rows in spread order: T - I and M (Pairs); backward: M^T in M's place, and T^T - I (fp32)
-    float *TT;
-    float *dec;             // per chunk: e^G, e^{G_C - G}, beta
+    void *T;                // 64 x 64 images, rows in spread order: T - I (Pairs); backward also M^T and T^T - I (fp32)
+    float *MT, *TT;
+    float *dec;             // per chunk (kDec): e^G, e^{G_C - G}, beta, and G as the sum of two floats
 };
 
 template <class X, int DK, bool BWD>
@@ -99,60 +107,53 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     typedef typename X::E E;
     __shared__ double G[C];
     __shared__ float B[C];
-    __shared__ __attribute__((aligned(16))) float A[C][68], T[C][68];
+    __shared__ __attribute__((aligned(16))) float A[C][68];     // then T
     const Sizes &z = a.z;
     const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, h = lane >> 5, col = lane & 31;
     const int bh = blockIdx.y, n = tokens_of(z, z.chunk0 + blockIdx.x);
     const int64_t t0 = static_cast<int64_t>(z.chunk0 + blockIdx.x) * C;
     const size_t at = static_cast<size_t>(bh) * z.chunks + blockIdx.x;
+    const int ti = wave > 0 ? 1 : 0, tj = wave == 2 ? 1 : 0;
+    f32x16 kk = zero16(), qk = zero16();
     if (wave == 3) {
         const int64_t t = static_cast<int64_t>(bh) * z.N + t0 + lane;
         const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[t])) : 0.0, lane);
-        const float b = lane < n ? strength(a.beta[t]) : kBetaFloor;
+        const float b = lane < n ? strength(a.beta[t]) : kBetaFloor, hi = static_cast<float>(g);
         G[lane] = g;
         B[lane] = b;
-        float *dec = a.dec + at * 3 * C;
-        dec[lane] = expf(static_cast<float>(g));
+        float *dec = a.dec + at * kDec;
+        dec[lane] = expf(hi);
         dec[C + lane] = expf(static_cast<float>(__shfl(g, 63) - g));
         dec[2 * C + lane] = b;
-    }
-    for (int i = tid; i < C * 68; i += 256) (&T[0][0])[i] = 0.f;
-    __syncthreads();
-    if (wave < 3) {
-        const int ti = wave > 0 ? 1 : 0, tj = wave == 2 ? 1 : 0;
+        dec[3 * C + lane] = hi;
+        dec[4 * C + lane] = static_cast<float>(g - hi);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) A[2 * i + (lane >> 5)][32 + (lane & 31)] = 0.f;
+    } else {
         const E *Q = static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk, *K = static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk;
-        f32x16 kk = zero16(), qk = zero16();
 #pragma unroll
         for (int kb = 0; kb < DK / 16; ++kb) {
             const int k0 = 16 * kb + 8 * h;
-            const typename X::Exact ki = rows8<X>(K, 32 * ti + col, n, z.dk, k0), qi = rows8<X>(Q, 32 * ti + col, n, z.dk, k0);
-            const typename X::Exact kj = rows8<X>(K, 32 * tj + col, n, z.dk, k0);
+            const typename X::Exact ki = rows8<X>(K, 32 * ti + col, n, z.dk, k0), kj = rows8<X>(K, 32 * tj + col, n, z.dk, k0);
             kk = mma(ki, kj, kk);
-            qk = BWD ? mma(qi, kj, qk) : mma(kj, qi, qk);       // the image's row is the accumulator's column
+            if (BWD) qk = mma(rows8<X>(Q, 32 * ti + col, n, z.dk, k0), kj, qk);
         }
-        E *M = static_cast<E *>(a.M) + at * X::kPairPlanes * C * C;
-        float *MT = static_cast<float *>(a.M) + at * C * C;
+    }
+    __syncthreads();
+    if (wave < 3) {
+        float *MT = a.MT + at * C * C + (32 * tj + col) * C + 32 * ti;
+        const int j = 32 * tj + col;
 #pragma unroll
-        for (int g16 = 0; g16 < 2; ++g16) {
-            float m[8];
+        for (int e4 = 0; e4 < 4; ++e4) {
+            f32x4 m;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int row = acc_row(8 * g16 + e, h);
-                const int i = 32 * ti + (BWD ? row : col), j = 32 * tj + (BWD ? col : row);
-                m[e] = j <= i ? z.scale * expf(static_cast<float>(G[i] - G[j])) * qk[8 * g16 + e] : 0.f;
+            for (int e = 0; e < 4; ++e) {
+                const int i = 32 * ti + acc_row(4 * e4 + e, h);
+                const float D = j <= i ? expf(static_cast<float>(G[i] - G[j])) : 0.f;
+                m[e] = j <= i ? z.scale * D * qk[4 * e4 + e] : 0.f;
+                A[i][j] = j < i ? B[i] * D * kk[4 * e4 + e] : 0.f;
             }
-#pragma unroll
-            for (int i8 = 0; i8 < 2; ++i8) {
-                const f32x4 v = {m[4 * i8], m[4 * i8 + 1], m[4 * i8 + 2], m[4 * i8 + 3]};
-                const int k = spread(16 * g16 + 8 * i8 + 4 * h);
-                if (BWD) *reinterpret_cast<f32x4 *>(MT + (32 * tj + col) * C + 32 * ti + k) = v;
-                else put4_pair(M + (32 * ti + col) * C + 32 * tj + k, C * C, v);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int i = 32 * ti + acc_row(e, h), j = 32 * tj + col;
-            A[i][j] = j < i ? B[i] * expf(static_cast<float>(G[i] - G[j])) * kk[e] : 0.f;
+            if (BWD) *reinterpret_cast<f32x4 *>(MT + spread(acc_row(4 * e4, h))) = m;
         }
     }
     __syncthreads();
@@ -166,24 +167,32 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
             for (int j = 0; j < i; ++j) s -= A[b0 + i][b0 + j] * x[j];
             x[i] = s;
         }
+        // (all of the wavefront has read its block)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) T[b0 + i][b0 + c16] = x[i];
+        for (int i = 0; i < 16; ++i) A[b0 + i][b0 + c16] = x[i];
     }
     __syncthreads();
-    if (wave < 2) merge_blocks<16>(A, T, 32 * wave, 0, lane);
+    if (wave < 2) {
+        MergeBlocks<16> m;
+        m.form(A, 32 * wave, 0, lane);
+        m.put(A, 32 * wave, 0, lane);
+    }
     __syncthreads();
-    if (wave < 2) merge_blocks<32>(A, T, 0, wave, lane);
+    MergeBlocks<32> m;
+    if (wave < 2) m.form(A, 0, wave, lane);
+    __syncthreads();            // both halves have been read
+    if (wave < 2) m.put(A, 0, wave, lane);
     __syncthreads();
-    for (int task = tid; task < C * 16; task += 256) {
-        const int row = task >> 4, k = 4 * (task & 15);
-        const size_t to = at * X::kPairPlanes * C * C + row * C + spread(k);
-        f32x4 v, w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int task = tid + 256 * i, row = task >> 4, k = 4 * (task & 15);
+        f32x4 v = *reinterpret_cast<const f32x4 *>(&A[row][k]), w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[e] = k + e == row ? 0.f : T[row][k + e];
-            w[e] = k + e == row ? 0.f : T[k + e][row];
+            if (k + e == row) v[e] = 0.f;
+            w[e] = k + e == row || !BWD ? 0.f : A[k + e][row];
         }
-        put4_pair(static_cast<E *>(a.T) + to, C * C, v);
+        put4_pair(static_cast<E *>(a.T) + at * X::kPairPlanes * C * C + row * C + spread(k), C * C, v);
         if (BWD) *reinterpret_cast<f32x4 *>(a.TT + at * C * C + row * C + spread(k)) = w;
     }
 }
@@ -395,7 +404,7 @@ enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's tran
 
 struct ScanArgs {
     Sizes z;
-    const void *Q, *K, *V, *T, *M;
+    const void *Q, *K, *V, *T;
     const float *dec;
     const float *start;             // state at the start of a segment, (dk, dv) fp32: start + bh * start_head + segment * dk * dv; null: zero
     size_t start_head;
@@ -443,10 +452,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     }
     constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
     RowsStage<X, DK> rows;
-    PairStage<THREADS> is, ms;
+    PairStage<THREADS> is;
     ColumnsStage<X> vs;
     const typename X::Exact unit = ColumnsStage<X>::unit(z.dv, 16 * tile, lane);
-    float ds = 0.f;
+    float ds[(kDec + THREADS - 1) / THREADS];
     auto take = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
         const int n = tokens_of(z, z.chunk0 + c);
@@ -454,9 +463,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
         if (kAhead) {
             is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
-            if (MODE == kOut) ms.take(static_cast<const E *>(a.M) + at * X::kPairPlanes * C * C, tid);
         }
-        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
+#pragma unroll
+        for (int i = 0; i < (kDec + THREADS - 1) / THREADS; ++i)
+            if (tid + THREADS * i < kDec) ds[i] = a.dec[at * kDec + tid + THREADS * i];
     };
     auto take_columns = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -465,6 +475,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     if (c0 < c1) {
         take(c0);
         if (active) take_columns(c0);
+    }
+    if (MODE == kOut && tid < 256) {        // what M's tiles leave out of the steps of 32 tokens on the diagonal
+        const int t = 2 * (tid >> 7), row = 16 * t + (tid >> 2 & 15), plane = tid >> 6 & 1;
+        if (plane < X::kPairPlanes) put4_zero(Ms + plane * L::kSquare + row * L::kTok + spread(16 * t + 16 + 4 * (tid & 3)));
     }
     for (int c = c0; c < c1; ++c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -475,15 +489,26 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (has_q) rows.template put<true, false>(n, z.dk, Qs, nullptr, task);
         if (!kAhead) is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
         is.template put<X>(Ts, tid);
-        if (MODE == kOut) {
-            if (!kAhead) ms.take(static_cast<const E *>(a.M) + at * X::kPairPlanes * C * C, tid);
-            ms.template put<X>(Ms, tid);
-        }
-        if (tid < 3 * C) dec[tid] = ds;
+#pragma unroll
+        for (int i = 0; i < (kDec + THREADS - 1) / THREADS; ++i)
+            if (tid + THREADS * i < kDec) dec[tid + THREADS * i] = ds[i];
         __syncthreads();
         if (c + 1 < c1) take(c + 1);
-        if (!active) continue;
         const float *eG = dec, *eEnd = dec + C, *beta = dec + 2 * C;
+        if (MODE == kOut) {         // M, a tile on or below the diagonal after the other: rows j, columns i
+            for (int t = wave; t < 10; t += THREADS / 64) {
+                const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2, i = 16 * ti + col, j0 = 16 * tj + 4 * q;
+                f32x4 m = zero4();
+#pragma unroll
+                for (int kb = 0; kb < DK / 32; ++kb) m = mma(tile8<X, L::kRow>(Ks, 16 * tj, 32 * kb, lane), tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), m);
+                const float hi = dec[3 * C + i], lo = dec[4 * C + i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m[e] = j0 + e <= i ? z.scale * expf((hi - dec[3 * C + j0 + e]) + (lo - dec[4 * C + j0 + e])) * m[e] : 0.f;
+                put4_pair(Ms + i * L::kTok + spread(j0), L::kSquare, m);
+            }
+            fence();
+        }
+        if (!active && MODE != kOut) continue;
         fence();
         // K S, and Q S for the outputs
         f32x4 R[4], O[4];
@@ -513,7 +538,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
                 if (MODE == kOut) O[ti][e] *= z.scale * g[e];
             }
         }
-        if (c + 1 < c1) take_columns(c + 1);
+        if (active && c + 1 < c1) take_columns(c + 1);
         fence();
         // U = T R = R + (T - I) R, and the outputs' M U
         f32x4 U[4];
@@ -527,6 +552,8 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
             for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Pair, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
         }
         if (MODE == kOut) {
+            __syncthreads();
+            if (!active) continue;
             E *out = static_cast<E *>(a.O) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
@@ -730,7 +757,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
             is.take(a.TT + at * C * C, tid);
             ms.take(a.MT + at * C * C, tid);
         }
-        if (tid < 3 * C) ds = a.dec[at * 3 * C + tid];
+        if (tid < 3 * C) ds = a.dec[at * kDec + tid];
     };
     auto take_columns = [&](int c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -1231,7 +1258,7 @@ template <class X, int DK>
 constexpr size_t scan_lds(bool out)
 {
     typedef Lds<X, DK> L;
-    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPairPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + 3 * C * sizeof(float);
+    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPairPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + kDec * sizeof(float);
 }
 template <class X, int DK>
 constexpr size_t rev_lds()
@@ -1276,7 +1303,7 @@ struct Passes {
     static constexpr int kTiles = THREADS / 64;
     static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
     {
-        PrepArgs a{z, io.Q, io.K, io.g, io.beta, ws + p.off_T, ws + p.off_M, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
+        PrepArgs a{z, io.Q, io.K, io.g, io.beta, ws + p.off_T, bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
         const dim3 grid(z.chunks, p.BH);
         if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
         else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
@@ -1290,7 +1317,6 @@ struct Passes {
         a.K = io.K;
         a.V = io.V;
         a.T = ws + p.off_T;
-        a.M = ws + p.off_M;
         a.dec = floats(ws, p.off_dec);
         return a;
     }
@@ -1442,7 +1468,7 @@ struct Passes {
             r.K = io.K;
             r.dO = io.dO;
             r.TT = floats(ws, p.off_TT);
-            r.MT = floats(ws, p.off_M);
+            r.MT = floats(ws, p.off_MT);
             r.dec = floats(ws, p.off_dec);
             RevArgs full = r;
             full.end = dcarry;

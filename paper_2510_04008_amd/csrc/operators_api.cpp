@@ -77,7 +77,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         return RACE_OK;
     }
     const size_t dkp = d->dk <= 64 ? 64 : 128, split = d->dtype == RACE_F32 ? 4 : 6, one = sizeof(float) * p.dk * p.dv, square = kChunk * kChunk;
-    const size_t per_chunk = square * 8 + 3 * kChunk * 4 + (backward ? square * 4 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
+    const size_t per_chunk = square * 4 + 5 * kChunk * 4 + (backward ? square * 8 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
     const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
         p.seg_chunks = static_cast<int>(std::min<int64_t>((d->chunk + kChunk - 1) / kChunk, p.chunks));
@@ -98,8 +98,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         return was;
     };
     p.off_T = take(n * square * 4);
-    p.off_M = take(n * square * 4);
-    p.off_dec = take(n * 3 * kChunk * sizeof(float));
+    p.off_dec = take(n * 5 * kChunk * sizeof(float));
     const size_t segs = static_cast<size_t>(p.BH) * p.nseg;
     if (p.win_segs > 1) {
         p.off_add = take(segs * one);
@@ -116,6 +115,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     if (p.windows > 1) p.off_carry = take(p.BH * one);
     if (backward) {
         if (p.win_segs > 1) p.off_end = take(segs * one);
+        p.off_MT = take(n * square * 4);
         p.off_TT = take(n * square * 4);
         p.off_S = take((n + p.BH) * dkp * p.dvp * 4);
         p.off_U = take(n * kChunk * p.dvp * 4);
