@@ -610,7 +610,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 }
 
 // ------------------------------------------------------------------ states at the segments' starts
-// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 columns, a
+// S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 COLS columns, a
 // wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
 // asked for two steps ahead.  A step takes 2 to 3 us all the same, most of it P on its way, so many segments are joined in groups of about the root of
 // their number: the transitions of the groups side by side (compose), the groups one after the other, then the segments of all groups side by side.
@@ -631,58 +631,77 @@ struct CombineArgs {
     size_t out_head;
 };
 
-template <class X, int DK, bool REV>
+template <class X, int DK, int COLS, bool REV>
 __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 {
     typedef typename X::E E;
     typedef typename X::Split Split;
-    __shared__ __attribute__((aligned(16))) E ops[2][X::kPlanes][DK / 32][64 * 8];
+    __shared__ __attribute__((aligned(16))) E ops[2][COLS][X::kPlanes][DK / 32][64 * 8];
     const Sizes &z = a.z;
     // workgroups go to the eight XCDs in turn: those of one head and group to the same one, whose L2 then fetches P once
-    const int vtiles = z.dvp / 16, tiles = vtiles + (a.out_P ? DK / 16 : 0), slot = blockIdx.x >> 3, unit = slot / tiles * 8 + (blockIdx.x & 7);
+    const int vtiles = z.dvp / 16 / COLS, tiles = vtiles + (a.out_P ? DK / 16 / COLS : 0), slot = blockIdx.x >> 3, unit = slot / tiles * 8 + (blockIdx.x & 7);
     if (unit >= a.heads * a.groups) return;
     const int bh = unit / a.groups, group = unit - bh * a.groups, tile = slot % tiles;
     const int begin = group * a.each, end = min(begin + a.each, a.steps);
-    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col = 16 * tile + (lane & 15);
+    const int wave = wave_index(), lane = threadIdx.x & 63, q = lane >> 4, col0 = 16 * COLS * tile + (lane & 15);
     const bool trans = tile >= vtiles;
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
     auto segment = [&](int i) { return REV ? a.first - i : a.first + i; };
     struct Step {
         Split P[DK / 32];
-        f32x4 B[1];
+        f32x4 B[COLS];
     } ahead[2];
-    f32x4 S[1] = {zero4()};
+    f32x4 S[COLS];
+#pragma unroll
+    for (int n = 0; n < COLS; ++n) S[n] = zero4();
+    auto get = [&](f32x4 (&to)[COLS], const float *state) {
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) get_state(reinterpret_cast<f32x4 (&)[1]>(to[n]), state, z.dk, z.dv, wave, col0 + 16 * n, lane);
+    };
+    auto put_to = [&](float *state) {
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) put_state(reinterpret_cast<f32x4 (&)[1]>(S[n]), state, z.dk, z.dv, wave, col0 + 16 * n, lane);
+    };
     auto take = [&](int i, Step &to) {
         const size_t s = static_cast<size_t>(bh) * a.p_head + segment(i);
         const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + state_row(wave, lane >> 2 & 3, lane & 3) * DK + 8 * q;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, to.P[kb]);
-        to.B[0] = zero4();
-        if (!trans) get_state(to.B, a.add + s * one, z.dk, z.dv, wave, col, lane);
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) to.B[n] = zero4();
+        if (!trans) get(to.B, a.add + s * one);
     };
     auto put = [&](int i) {
-        if (a.at) put_state(S, a.at + bh * a.at_head + segment(i) * one, z.dk, z.dv, wave, col, lane);
+        if (a.at) put_to(a.at + bh * a.at_head + segment(i) * one);
     };
-    auto step = [&](int i, Step &my, E (*op)[DK / 32][64 * 8]) {
+    auto step = [&](int i, Step &my, E (*op)[X::kPlanes][DK / 32][64 * 8]) {
         put(i);
         // the lane's four rows are half of its eight places in the operand of 32 rows
-        put4(&op[0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[0]);
-        f32x4 sums[2] = {my.B[0], zero4()};
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) put4(&op[n][0][wave >> 1][lane * 8 + 4 * (wave & 1)], DK / 32 * 64 * 8, S[n]);
+        f32x4 sums[COLS][2];
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) sums[n][0] = my.B[n], sums[n][1] = zero4();
         __syncthreads();
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) {
-            Split s;
-            get8(&op[0][kb][lane * 8], DK / 32 * 64 * 8, s);
-            sums[kb & 1] = mma(my.P[kb], s, sums[kb & 1]);
-        }
-        S[0] = sums[0] + sums[1];
+        for (int kb = 0; kb < DK / 32; ++kb)
+#pragma unroll
+            for (int n = 0; n < COLS; ++n) {
+                Split s;
+                get8(&op[n][0][kb][lane * 8], DK / 32 * 64 * 8, s);
+                sums[n][kb & 1] = mma(my.P[kb], s, sums[n][kb & 1]);
+            }
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) S[n] = sums[n][0] + sums[n][1];
         if (i + 2 < end) take(i + 2, my);
     };
     if (trans) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[0][e] = state_row(wave, q, e) == col - z.dvp ? 1.f : 0.f;
+        for (int n = 0; n < COLS; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[n][e] = state_row(wave, q, e) == col0 + 16 * n - z.dvp ? 1.f : 0.f;
     } else if (a.carry) {
-        get_state(S, a.carry + bh * a.carry_head + group * a.carry_group, z.dk, z.dv, wave, col, lane);
+        get(S, a.carry + bh * a.carry_head + group * a.carry_group);
     }
     if (begin < end) take(begin, ahead[0]);
     if (begin + 1 < end) take(begin + 1, ahead[1]);
@@ -695,9 +714,11 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
         if (trans) {
             E *P = static_cast<E *>(a.out_P) + g * X::kPlanes * DK * DK;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) put1(P + state_row(wave, q, e) * DK + col - z.dvp, DK * DK, S[0][e]);
+            for (int n = 0; n < COLS; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) put1(P + state_row(wave, q, e) * DK + col0 + 16 * n - z.dvp, DK * DK, S[n][e]);
         } else {
-            put_state(S, a.out_add + g * one, z.dk, z.dv, wave, col, lane);
+            put_to(a.out_add + g * one);
         }
     } else if (group == a.groups - 1) {
         put(a.steps);
@@ -1383,9 +1404,15 @@ struct Passes {
     }
     static hipError_t launch_combine(const CombineArgs &a, bool rev, hipStream_t st)
     {
-        const int tiles = a.z.dvp / 16 + (a.out_P ? DK / 16 : 0), grid = (a.heads * a.groups + 7) / 8 * 8 * tiles;
-        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, true>), grid, 4 * DK, 0, st, a);
-        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, false>), grid, 4 * DK, 0, st, a);
+        // one chain of steps: as few columns as there are workgroups for; several side by side: P read half as often
+        return a.groups == 1 && !a.out_P ? launch_columns<1>(a, rev, st) : launch_columns<2>(a, rev, st);
+    }
+    template <int COLS>
+    static hipError_t launch_columns(const CombineArgs &a, bool rev, hipStream_t st)
+    {
+        const int tiles = (a.z.dvp / 16 + (a.out_P ? DK / 16 : 0)) / COLS, grid = (a.heads * a.groups + 7) / 8 * 8 * tiles;
+        if (rev) DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, COLS, true>), grid, 4 * DK, 0, st, a);
+        else DELTA_LAUNCH("delta_join", (delta_combine_kernel<X, DK, COLS, false>), grid, 4 * DK, 0, st, a);
         return hipSuccess;
     }
 
