@@ -350,6 +350,12 @@ __device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 *
 __device__ __forceinline__ float gate(float g) { return g < kGateFloor ? kGateFloor : g; }       // NaN stays
 __device__ __forceinline__ float strength(float b) { return fabsf(b) < kBetaFloor ? kBetaFloor : b; }
 
+// exp(G_i - G_j) of sums that are held as two floats each: their difference is exact to fp32 however large they are
+__device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float lo_j)
+{
+    return __builtin_amdgcn_exp2f(((hi_i - hi_j) + (lo_i - lo_j)) * 1.44269504088896f);
+}
+
 // running sum over the 64 lanes
 __device__ __forceinline__ double prefix64(double x, int lane)
 {

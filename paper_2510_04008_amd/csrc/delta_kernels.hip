@@ -105,8 +105,7 @@ template <class X, int DK, bool BWD>
 __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
 {
     typedef typename X::E E;
-    __shared__ double G[C];
-    __shared__ float B[C];
+    __shared__ __attribute__((aligned(16))) float B[C], hi_of[C], lo_of[C];
     __shared__ __attribute__((aligned(16))) float A[C][68];     // then T
     const Sizes &z = a.z;
     const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, h = lane >> 5, col = lane & 31;
@@ -119,7 +118,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
         const int64_t t = static_cast<int64_t>(bh) * z.N + t0 + lane;
         const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[t])) : 0.0, lane);
         const float b = lane < n ? strength(a.beta[t]) : kBetaFloor, hi = static_cast<float>(g);
-        G[lane] = g;
+        hi_of[lane] = hi;
+        lo_of[lane] = static_cast<float>(g - hi);
         B[lane] = b;
         float *dec = a.dec + at * kDec;
         dec[lane] = expf(hi);
@@ -143,15 +143,17 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     if (wave < 3) {
         float *MT = a.MT + at * C * C + (32 * tj + col) * C + 32 * ti;
         const int j = 32 * tj + col;
+        const float hj = hi_of[j], lj = lo_of[j];
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
+            const int i0 = 32 * ti + acc_row(4 * e4, h);
+            const f32x4 hi = *reinterpret_cast<const f32x4 *>(hi_of + i0), lo = *reinterpret_cast<const f32x4 *>(lo_of + i0), b = *reinterpret_cast<const f32x4 *>(B + i0);
             f32x4 m;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = 32 * ti + acc_row(4 * e4 + e, h);
-                const float D = j <= i ? expf(static_cast<float>(G[i] - G[j])) : 0.f;
-                m[e] = j <= i ? z.scale * D * qk[4 * e4 + e] : 0.f;
-                A[i][j] = j < i ? B[i] * D * kk[4 * e4 + e] : 0.f;
+                const float D = decay(hi[e], lo[e], hj, lj), x = z.scale * D * qk[4 * e4 + e], y = b[e] * D * kk[4 * e4 + e];
+                m[e] = j <= i0 + e ? x : 0.f;
+                A[i0 + e][j] = j < i0 + e ? y : 0.f;
             }
             if (BWD) *reinterpret_cast<f32x4 *>(MT + spread(acc_row(4 * e4, h))) = m;
         }
@@ -502,8 +504,12 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 #pragma unroll
                 for (int kb = 0; kb < DK / 32; ++kb) m = mma(tile8<X, L::kRow>(Ks, 16 * tj, 32 * kb, lane), tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), m);
                 const float hi = dec[3 * C + i], lo = dec[4 * C + i];
+                const f32x4 hj = *reinterpret_cast<const f32x4 *>(dec + 3 * C + j0), lj = *reinterpret_cast<const f32x4 *>(dec + 4 * C + j0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m[e] = j0 + e <= i ? z.scale * expf((hi - dec[3 * C + j0 + e]) + (lo - dec[4 * C + j0 + e])) * m[e] : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    const float x = z.scale * decay(hi, lo, hj[e], lj[e]) * m[e];
+                    m[e] = j0 + e <= i ? x : 0.f;
+                }
                 put4_pair(Ms + i * L::kTok + spread(j0), L::kSquare, m);
             }
             fence();
@@ -881,8 +887,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 struct GradArgs {
     Sizes z;
     const void *Q, *K, *V, *dO;
-    const float *g, *beta;
-    const float *S, *U, *dS, *dR;
+    const float *dec, *S, *U, *dS, *dR;
     void *dQ, *dK;                  // the caller's tensors, or with `shared` fp32 (BH, 64 chunks, dk) parts
     int shared;
     float *dg, *dbeta;
@@ -926,9 +931,9 @@ struct GradLds {
     typedef Lds<X, DK> L;
     static constexpr int kWide = 128 + X::kPad;                         // a token's row over columns of the state, in spread order
     static constexpr bool kHasO = sizeof(E) == 2;                       // dO has no room beside fp32 tiles: its operands come from memory
-    static constexpr int kFloats = 3 * C + 8 * C + C + 8;               // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
+    static constexpr int kFloats = kDec + 8 * C + C + 8;                // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
     static constexpr int kTiles = C * kWide * (X::kPlanes + X::kPairPlanes + (kHasO ? 1 : 0));
-    static constexpr size_t kBytes = C * sizeof(double) + kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
+    static constexpr size_t kBytes = kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
     static_assert((X::kPlanes + 2 * X::kPairPlanes) * L::kSquare <= kTiles, "F, F^T and E + E^T lie where U, dR and dO were");
 };
 
@@ -943,8 +948,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     typedef GradLds<X, DK> G;
     constexpr int kWide = G::kWide, kTok = L::kTok, TI = DK / 32;       // TI: 16-token tiles of a wavefront
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    double *Gs = reinterpret_cast<double *>(lds_raw);
-    float *eG = reinterpret_cast<float *>(Gs + C), *eEnd = eG + C, *bs = eEnd + C, *qd = bs + C, *vd = qd + 8 * C, *part = vd + C;
+    float *eG = reinterpret_cast<float *>(lds_raw), *eEnd = eG + C, *bs = eEnd + C, *hi_of = bs + C, *lo_of = hi_of + C, *qd = lo_of + C, *vd = qd + 8 * C, *part = vd + C;
     E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPairPlanes * C * kWide;
     E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
     const Sizes &z = a.z;
@@ -959,48 +963,54 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     const int deep = z.dvp / 32;            // steps of a product over the state's columns
     const int dcol = 16 * (wave % (DK / 16)) + col, ti0 = wave / (DK / 16) * TI;
 
-    if (wave == 7) {
-        const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[row0 + lane])) : 0.0, lane);
-        Gs[lane] = g;
-        eG[lane] = expf(static_cast<float>(g));
-        eEnd[lane] = expf(static_cast<float>(__shfl(g, 63) - g));
-        bs[lane] = lane < n ? strength(a.beta[row0 + lane]) : kBetaFloor;
-    }
-    for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
-    {
-        RowsStage<X, DK> rows;
-        const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
-        const int task = has_k ? tid : tid - (kGradThreads - 2 * DK);
-        if (has_k || has_q) {
-            rows.take(has_k ? K : Q, n, z.dk, task);
-            rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
-        }
-    }
-    // the tiles, and on the way u.dR and v.dR of every token: 16 lanes a row, eight places each
+    // everything is asked for at once, in the order in which it is used
+    RowsStage<X, DK> rows;
+    const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
+    const int task = has_k ? tid : tid - (kGradThreads - 2 * DK);
+    if (has_k || has_q) rows.take(has_k ? K : Q, n, z.dk, task);
+    if (tid < kDec) eG[tid] = a.dec[at * kDec + tid];
+    const int p0 = 8 * (tid & 15);          // 16 lanes a token, eight places each
+    float u[2][8], r[2][8];
+    Exact v[2], o[2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const int i = (tid >> 4) + 32 * half, p = 8 * (tid & 15);
-        float u[8], r[8], v[8], ud = 0.f, vr = 0.f;
-        const bool there = p < z.dvp;
+        const int i = (tid >> 4) + 32 * half;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = r[e] = 0.f;
-        if (there) {
-            kept8(U + i * z.dvp + p, u);
-            kept8(dR + i * z.dvp + p, r);
+        for (int e = 0; e < 8; ++e) u[half][e] = r[half][e] = 0.f;
+        if (p0 < z.dvp) {
+            kept8(U + i * z.dvp + p0, u[half]);
+            kept8(dR + i * z.dvp + p0, r[half]);
         }
-        values8(rows8_spread<X>(V, i, there ? n : 0, z.dv, p), v);
-        const Exact o = rows8_spread<X>(dO, i, there ? n : 0, z.dv, p);
+        v[half] = rows8_spread<X>(V, i, p0 < z.dvp ? n : 0, z.dv, p0);
+        o[half] = rows8_spread<X>(dO, i, p0 < z.dvp ? n : 0, z.dv, p0);
+    }
+    float s[4][8], d[4][8], dot = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+        if (kb < deep) {
+            kept8(S + dcol * z.dvp + 32 * kb + 8 * q, s[kb]);
+            kept8(dS + dcol * z.dvp + 32 * kb + 8 * q, d[kb]);
+        }
+    for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
+    if (has_k || has_q) rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
+    __syncthreads();                        // the strengths
+    // the tiles, and on the way u.dR and v.dR of every token
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int i = (tid >> 4) + 32 * half;
         Split us;
         Pair rs;
-        split8(u, us);
-        split8(r, rs);
-        put8(Us + i * kWide + p, C * kWide, us);
-        put8(Rs + i * kWide + p, C * kWide, rs);
-        if (G::kHasO) put8(Os + i * kWide + p, o);
+        split8(u[half], us);
+        split8(r[half], rs);
+        put8(Us + i * kWide + p0, C * kWide, us);
+        put8(Rs + i * kWide + p0, C * kWide, rs);
+        if (G::kHasO) put8(Os + i * kWide + p0, o[half]);
+        float x[8], ud = 0.f, vr = 0.f;
+        values8(v[half], x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            ud += u[e] * r[e];
-            vr += v[e] * r[e];
+            ud += u[half][e] * r[half][e];
+            vr += x[e] * r[half][e];
         }
 #pragma unroll
         for (int m = 1; m < 16; m *= 2) {
@@ -1008,9 +1018,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
             vr += __shfl_xor(vr, m);
         }
         if ((tid & 15) == 0) {
-            const float b = i < n ? strength(a.beta[row0 + i]) : kBetaFloor;
-            vd[i] = b * vr;
-            if (i < n) a.dbeta[row0 + i] = ud / b;
+            vd[i] = bs[i] * vr;
+            if (i < n) a.dbeta[row0 + i] = ud / bs[i];
         }
     }
     __syncthreads();
@@ -1047,20 +1056,18 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     f32x4 dq[TI], dk[TI], y[TI];
 #pragma unroll
     for (int t = 0; t < TI; ++t) dq[t] = dk[t] = y[t] = zero4();
-    float dot = 0.f;
-#pragma unroll 1
-    for (int kb = 0; kb < deep; ++kb) {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+        if (kb >= deep) continue;
         const int p = 32 * kb;
-        float s[8], d[8], s1[8];
-        kept8(S + dcol * z.dvp + p + 8 * q, s);
-        kept8(dS + dcol * z.dvp + p + 8 * q, d);
+        float s1[8];
         kept8(S + (DK + dcol) * z.dvp + p + 8 * q, s1);
         Split ss;
         Pair ds;
-        split8(s, ss);
-        split8(d, ds);
+        split8(s[kb], ss);
+        split8(d[kb], ds);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot += s1[e] * d[e];
+        for (int e = 0; e < 8; ++e) dot += s1[e] * d[kb][e];
 #pragma unroll
         for (int t = 0; t < TI; ++t) {
             const int row = 16 * (ti0 + t);
@@ -1091,9 +1098,11 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         if (job >= 20) continue;
         const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
         const int i = 16 * ti + col, j0 = 16 * tj + 4 * q;
+        const float hi = hi_of[i], lo = lo_of[i];
+        const f32x4 hj = *reinterpret_cast<const f32x4 *>(hi_of + j0), lj = *reinterpret_cast<const f32x4 *>(lo_of + j0);
         f32x4 D;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) D[e] = j0 + e <= i ? expf(static_cast<float>(Gs[i] - Gs[j0 + e])) : 0.f;
+        for (int e = 0; e < 4; ++e) D[e] = decay(hi, lo, hj[e], lj[e]);
         if (job < 10) {
             const f32x4 f = z.scale * D * jobs[k];
             f32x4 f0;
@@ -1522,7 +1531,7 @@ struct Passes {
             }
             const float *a_S = floats(ws, p.off_S), *a_U = floats(ws, p.off_U);
             const bool shared = p.H != p.Hk;
-            GradArgs g{z, io.Q, io.K, io.V, io.dO, io.g, io.beta, a_S, a_U, full.dS, full.dR,
+            GradArgs g{z, io.Q, io.K, io.V, io.dO, r.dec, a_S, a_U, full.dS, full.dR,
                        shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta};
             DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3(z.chunks, p.BH), kGradThreads, (GradLds<X, DK>::kBytes), st, g);
             if (shared) {
