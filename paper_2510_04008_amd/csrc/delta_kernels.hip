@@ -891,6 +891,7 @@ struct GradArgs {
     void *dQ, *dK;                  // the caller's tensors, or with `shared` fp32 (BH, 64 chunks, dk) parts
     int shared;
     float *dg, *dbeta;
+    int each;                       // chunks of a workgroup
 };
 
 // the elements of a caller's row at eight places of the spread order, from place p (a multiple of 8)
@@ -952,256 +953,290 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPairPlanes * C * kWide;
     E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
     const Sizes &z = a.z;
-    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, q = lane >> 4, col = lane & 15;
-    const int bh = blockIdx.y, c = blockIdx.x, n = tokens_of(z, z.chunk0 + c);
-    const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
-    const size_t at = static_cast<size_t>(bh) * z.chunks + c;
-    const E *K = static_cast<const E *>(a.K) + qk_row(z, bh, t0) * z.dk, *Q = static_cast<const E *>(a.Q) + qk_row(z, bh, t0) * z.dk;
-    const E *V = static_cast<const E *>(a.V) + row0 * z.dv, *dO = static_cast<const E *>(a.dO) + row0 * z.dv;
-    const float *S = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, *dS = a.dS + at * DK * z.dvp;
-    const float *U = a.U + at * C * z.dvp, *dR = a.dR + at * C * z.dvp;
+    const int wave = wave_index();
+    int tid = threadIdx.x;
+    int lane = tid & 63, q = lane >> 4, col = lane & 15;
+    const int bh = blockIdx.y, c_low = blockIdx.x * a.each, c_high = min(c_low + a.each, z.chunks);
+    const float *S0 = a.S + static_cast<size_t>(bh) * (z.chunks + 1) * DK * z.dvp;
     const int deep = z.dvp / 32;            // steps of a product over the state's columns
-    const int dcol = 16 * (wave % (DK / 16)) + col, ti0 = wave / (DK / 16) * TI;
+    int dcol = 16 * (wave % (DK / 16)) + col;
+    const int ti0 = wave / (DK / 16) * TI;
 
-    // everything is asked for at once, in the order in which it is used
+    // what a chunk reads: asked for at once, and while the products of the chunk before are formed
     RowsStage<X, DK> rows;
-    const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
-    const int task = has_k ? tid : tid - (kGradThreads - 2 * DK);
-    if (has_k || has_q) rows.take(has_k ? K : Q, n, z.dk, task);
-    if (tid < kDec) eG[tid] = a.dec[at * kDec + tid];
-    const int p0 = 8 * (tid & 15);          // 16 lanes a token, eight places each
-    float u[2][8], r[2][8];
+    float u[2][8], r[2][8], s[4][8], d[4][8], s1[4][8], decs = 0.f;
     Exact v[2], o[2];
+    auto take_state = [&](const float *from, float (&to)[4][8]) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int i = (tid >> 4) + 32 * half;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[half][e] = r[half][e] = 0.f;
-        if (p0 < z.dvp) {
-            kept8(U + i * z.dvp + p0, u[half]);
-            kept8(dR + i * z.dvp + p0, r[half]);
-        }
-        v[half] = rows8_spread<X>(V, i, p0 < z.dvp ? n : 0, z.dv, p0);
-        o[half] = rows8_spread<X>(dO, i, p0 < z.dvp ? n : 0, z.dv, p0);
-    }
-    float s[4][8], d[4][8], dot = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-        if (kb < deep) {
-            kept8(S + dcol * z.dvp + 32 * kb + 8 * q, s[kb]);
-            kept8(dS + dcol * z.dvp + 32 * kb + 8 * q, d[kb]);
-        }
-    for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
-    if (has_k || has_q) rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
-    __syncthreads();                        // the strengths
-    // the tiles, and on the way u.dR and v.dR of every token
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int i = (tid >> 4) + 32 * half;
-        Split us;
-        Pair rs;
-        split8(u[half], us);
-        split8(r[half], rs);
-        put8(Us + i * kWide + p0, C * kWide, us);
-        put8(Rs + i * kWide + p0, C * kWide, rs);
-        if (G::kHasO) put8(Os + i * kWide + p0, o[half]);
-        float x[8], ud = 0.f, vr = 0.f;
-        values8(v[half], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ud += u[half][e] * r[half][e];
-            vr += x[e] * r[half][e];
-        }
-#pragma unroll
-        for (int m = 1; m < 16; m *= 2) {
-            ud += __shfl_xor(ud, m);
-            vr += __shfl_xor(vr, m);
-        }
-        if ((tid & 15) == 0) {
-            vd[i] = bs[i] * vr;
-            if (i < n) a.dbeta[row0 + i] = ud / bs[i];
-        }
-    }
-    __syncthreads();
-    // rows of the left operands: 16 tokens of a tile, 32 places from p
-    auto tokens_o = [&](int row, int p) -> Exact {
-        if (G::kHasO) return get8(Os + (row + col) * kWide + p + 8 * q);
-        return rows8_spread<X>(dO, row + col, n, z.dv, p + 8 * q);
+        for (int kb = 0; kb < 4; ++kb)
+            if (kb < deep) kept8(from + dcol * z.dvp + 32 * kb + 8 * q, to[kb]);
     };
+    auto take = [&](int c) {
+        const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
+        const int task = has_k ? tid : tid - (kGradThreads - 2 * DK), p0 = 8 * (tid & 15);          // 16 lanes a token, eight places each
+        const int n = tokens_of(z, z.chunk0 + c);
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
+        if (tid < kDec) decs = a.dec[at * kDec + tid];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = (tid >> 4) + 32 * half;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[half][e] = r[half][e] = 0.f;
+            if (p0 < z.dvp) {
+                kept8(a.U + (at * C + i) * z.dvp + p0, u[half]);
+                kept8(a.dR + (at * C + i) * z.dvp + p0, r[half]);
+            }
+            v[half] = rows8_spread<X>(static_cast<const E *>(a.V) + row0 * z.dv, i, p0 < z.dvp ? n : 0, z.dv, p0);
+            o[half] = rows8_spread<X>(static_cast<const E *>(a.dO) + row0 * z.dv, i, p0 < z.dvp ? n : 0, z.dv, p0);
+        }
+    };
+    auto take_states = [&](int c) {
+        take_state(S0 + static_cast<size_t>(c) * DK * z.dvp, s);
+        take_state(a.dS + (static_cast<size_t>(bh) * z.chunks + c) * DK * z.dvp, d);
+    };
+    take_state(S0 + static_cast<size_t>(c_high) * DK * z.dvp, s1);
+    if (c_low < c_high) take_states(c_high - 1);
+    for (int c = c_high - 1; c >= c_low; --c) {
+        // (what follows from the lane is formed anew for each chunk, not kept in registers)
+        asm volatile("" : "+v"(tid));
+        lane = tid & 63, q = lane >> 4, col = lane & 15, dcol = 16 * (wave % (DK / 16)) + col;
+        const int n = tokens_of(z, z.chunk0 + c);
+        const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C, row0 = static_cast<int64_t>(bh) * z.N + t0;
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        const E *dO = static_cast<const E *>(a.dO) + row0 * z.dv;
+        const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
+        const int task = has_k ? tid : tid - (kGradThreads - 2 * DK), p0 = 8 * (tid & 15);
+        take(c);
+        __syncthreads();                        // the chunk before is done with the tiles
+        if (tid < kDec) eG[tid] = decs;
+        for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
+        if (has_k || has_q) rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
+        __syncthreads();                        // the strengths
+        // the tiles, and on the way u.dR and v.dR of every token; over the states <S', dS>
+        float dot = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+            if (kb < deep) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot += s1[kb][e] * d[kb][e];
+            }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = (tid >> 4) + 32 * half;
+            fence();
+            Split us;
+            Pair rs;
+            split8(u[half], us);
+            split8(r[half], rs);
+            put8(Us + i * kWide + p0, C * kWide, us);
+            put8(Rs + i * kWide + p0, C * kWide, rs);
+            if (G::kHasO) put8(Os + i * kWide + p0, o[half]);
+            float x[8], ud = 0.f, vr = 0.f;
+            values8(v[half], x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ud += u[half][e] * r[half][e];
+                vr += x[e] * r[half][e];
+            }
+#pragma unroll
+            for (int m = 1; m < 16; m *= 2) {
+                ud += __shfl_xor(ud, m);
+                vr += __shfl_xor(vr, m);
+            }
+            if ((tid & 15) == 0) {
+                vd[i] = bs[i] * vr;
+                if (i < n) a.dbeta[row0 + i] = ud / bs[i];
+            }
+        }
+        __syncthreads();
+        // rows of the left operands: 16 tokens of a tile, 32 places from p
+        auto tokens_o = [&](int row, int p) -> Exact {
+            if (G::kHasO) return get8(Os + (row + col) * kWide + p + 8 * q);
+            return rows8_spread<X>(dO, row + col, n, z.dv, p + 8 * q);
+        };
 
-    // F (jobs 0 .. 9) and E (10 .. 19): 16 x 16 tiles on and below the diagonal; rows j, columns i
-    f32x4 jobs[3];
+        fence();
+        // F (jobs 0 .. 9) and E (10 .. 19): 16 x 16 tiles on and below the diagonal; rows j, columns i
+        f32x4 jobs[3];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        jobs[k] = zero4();
-        const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
-        if (job >= 20) continue;
-        const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
+        for (int k = 0; k < 3; ++k) {
+            jobs[k] = zero4();
+            const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
+            if (job >= 20) continue;
+            const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
 #pragma unroll 1
-        for (int kb = 0; kb < deep; ++kb) {
+            for (int kb = 0; kb < deep; ++kb) {
+                const int p = 32 * kb;
+                if (job < 10) {
+                    Split u;
+                    get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
+                    jobs[k] = mma(u, tokens_o(16 * ti, p), jobs[k]);
+                } else {
+                    Pair u, r;
+                    get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
+                    get8(Rs + (16 * ti + col) * kWide + p + 8 * q, C * kWide, r);
+                    jobs[k] = mma(u, r, jobs[k]);
+                }
+            }
+        }
+        // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T
+        f32x4 dq[TI], dk[TI], y[TI];
+#pragma unroll
+        for (int t = 0; t < TI; ++t) dq[t] = dk[t] = y[t] = zero4();
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            if (kb >= deep) continue;
             const int p = 32 * kb;
-            if (job < 10) {
-                Split u;
-                get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
-                jobs[k] = mma(u, tokens_o(16 * ti, p), jobs[k]);
-            } else {
+            fence();
+            Split ss;
+            Pair ds;
+            split8(s[kb], ss);
+            split8(d[kb], ds);
+#pragma unroll
+            for (int t = 0; t < TI; ++t) {
+                const int row = 16 * (ti0 + t);
+                fence();
                 Pair u, r;
-                get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
-                get8(Rs + (16 * ti + col) * kWide + p + 8 * q, C * kWide, r);
-                jobs[k] = mma(u, r, jobs[k]);
+                get8(Us + (row + col) * kWide + p + 8 * q, C * kWide, u);
+                get8(Rs + (row + col) * kWide + p + 8 * q, C * kWide, r);
+                dq[t] = mma(tokens_o(row, p), ss, dq[t]);
+                y[t] = mma(r, lead(ss), y[t]);
+                dk[t] = mma(u, ds, dk[t]);
             }
         }
-    }
-    // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T; over the states <S', dS>
-    f32x4 dq[TI], dk[TI], y[TI];
 #pragma unroll
-    for (int t = 0; t < TI; ++t) dq[t] = dk[t] = y[t] = zero4();
+        for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-        if (kb >= deep) continue;
-        const int p = 32 * kb;
-        float s1[8];
-        kept8(S + (DK + dcol) * z.dvp + p + 8 * q, s1);
-        Split ss;
-        Pair ds;
-        split8(s[kb], ss);
-        split8(d[kb], ds);
+            for (int e = 0; e < 8; ++e) s1[kb][e] = s[kb][e];
+        if (ti0 > 0) dot = 0.f;         // with dk <= 64 two wavefronts have met the same rows
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot += s1[e] * d[kb][e];
+        for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
+        if (lane == 0) part[wave] = dot;
 #pragma unroll
         for (int t = 0; t < TI; ++t) {
-            const int row = 16 * (ti0 + t);
-            Pair u, r;
-            get8(Us + (row + col) * kWide + p + 8 * q, C * kWide, u);
-            get8(Rs + (row + col) * kWide + p + 8 * q, C * kWide, r);
-            dq[t] = mma(tokens_o(row, p), ss, dq[t]);
-            y[t] = mma(r, lead(ss), y[t]);
-            dk[t] = mma(u, ds, dk[t]);
+            const int i = 16 * (ti0 + t) + 4 * q;
+            const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + i), b = *reinterpret_cast<const f32x4 *>(bs + i);
+            dq[t] *= z.scale * g;
+            dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b * g * y[t];
         }
-    }
-    if (ti0 > 0) dot = 0.f;         // with dk <= 64 two wavefronts have met the same rows
+        __syncthreads();
+        // F, its transpose, and E + E^T
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
-    if (lane == 0) part[wave] = dot;
+        for (int k = 0; k < 3; ++k) {
+            const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
+            if (job >= 20) continue;
+            const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
+            const int i = 16 * ti + col, j0 = 16 * tj + 4 * q;
+            const float hi = hi_of[i], lo = lo_of[i];
+            const f32x4 hj = *reinterpret_cast<const f32x4 *>(hi_of + j0), lj = *reinterpret_cast<const f32x4 *>(lo_of + j0);
+            f32x4 D;
 #pragma unroll
-    for (int t = 0; t < TI; ++t) {
-        const int i = 16 * (ti0 + t) + 4 * q;
-        const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + i), b = *reinterpret_cast<const f32x4 *>(bs + i);
-        dq[t] *= z.scale * g;
-        dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b * g * y[t];
-    }
-    __syncthreads();
-    // F, its transpose, and E + E^T
+            for (int e = 0; e < 4; ++e) D[e] = decay(hi, lo, hj[e], lj[e]);
+            if (job < 10) {
+                const f32x4 f = z.scale * D * jobs[k];
+                f32x4 f0;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
-        if (job >= 20) continue;
-        const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
-        const int i = 16 * ti + col, j0 = 16 * tj + 4 * q;
-        const float hi = hi_of[i], lo = lo_of[i];
-        const f32x4 hj = *reinterpret_cast<const f32x4 *>(hi_of + j0), lj = *reinterpret_cast<const f32x4 *>(lo_of + j0);
-        f32x4 D;
+                for (int e = 0; e < 4; ++e) f0[e] = j0 + e <= i ? f[e] : 0.f;
+                put4(F + i * kTok + spread(j0), L::kSquare, f0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) D[e] = decay(hi, lo, hj[e], lj[e]);
-        if (job < 10) {
-            const f32x4 f = z.scale * D * jobs[k];
-            f32x4 f0;
+                for (int e = 0; e < 4; ++e) put1_pair(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
+            } else {
+                const f32x4 x = -bs[i] * D * jobs[k];
+                f32x4 x0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f0[e] = j0 + e <= i ? f[e] : 0.f;
-            put4(F + i * kTok + spread(j0), L::kSquare, f0);
+                for (int e = 0; e < 4; ++e) x0[e] = j0 + e < i ? x[e] : 0.f;
+                put4_pair(Es + i * kTok + spread(j0), L::kSquare, x0);
+                // after the rows: in a diagonal tile these places hold its zeros
 #pragma unroll
-            for (int e = 0; e < 4; ++e) put1_pair(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
+                for (int e = 0; e < 4; ++e)
+                    if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, x[e]);
+            }
+        }
+        fence();
+        if (c > c_low) take_states(c - 1);
+        fence();
+        // what F and F^T have not: half of the steps of 32 tokens on the diagonal
+        if (wave >= 4) {
+            const int t = 2 * (wave & 1);
+            E *to = wave < 6 ? F + (16 * t + col) * kTok + spread(16 * t + 16 + 4 * q) : Ft + (16 * t + 16 + col) * kTok + spread(16 * t + 4 * q);
+            if (wave < 6) put4(to, L::kSquare, zero4());
+            else put4_pair(to, L::kSquare, zero4());
+        }
+        __syncthreads();
+        // dQ += F K, dK += F^T Q + (E + E^T) K
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int p = 32 * kb + 8 * q;
+            const Exact k = get8(Kt + dcol * kTok + p), qq = get8(Qt + dcol * kTok + p);
+#pragma unroll
+            for (int t = 0; t < TI; ++t) {
+                const int ti = ti0 + t;
+                Pair e;
+                get8(Es + (16 * ti + col) * kTok + p, L::kSquare, e);
+                dk[t] = mma(e, k, dk[t]);
+                if (ti >= 2 * kb) {         // F is lower triangular
+                    Split f;
+                    get8(F + (16 * ti + col) * kTok + p, L::kSquare, f);
+                    dq[t] = mma(f, k, dq[t]);
+                }
+                if (ti < 2 * kb + 2) {
+                    Pair f;
+                    get8(Ft + (16 * ti + col) * kTok + p, L::kSquare, f);
+                    dk[t] = mma(f, qq, dk[t]);
+                }
+            }
+        }
+        {
+            float v[4 * TI];
+#pragma unroll
+            for (int t = 0; t < TI; ++t) {
+                float x[4];
+                get4(Qt + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * dq[t][e];
+            }
+            const float s = sum_lanes<TI>(v, lane);
+            const int w = col % (4 * TI);
+            if (col < 4 * TI) qd[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
+        }
+        const int d0 = dcol - col;
+        if (a.shared) {
+            const buffer_t outq = buffer(static_cast<float *>(a.dQ) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+            const buffer_t outk = buffer(static_cast<float *>(a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
+#pragma unroll
+            for (int t = 0; t < TI; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int to = state_offset(16 * (ti0 + t) + 4 * q + e, z.dk, dcol);
+                    put_buffer(outq, to, dq[t][e]);
+                    put_buffer(outk, to, dk[t][e]);
+                }
         } else {
-            const f32x4 x = -bs[i] * D * jobs[k];
-            f32x4 x0;
+            E *outq = static_cast<E *>(a.dQ) + qk_row(z, bh, t0) * z.dk, *outk = static_cast<E *>(a.dK) + qk_row(z, bh, t0) * z.dk;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x0[e] = j0 + e < i ? x[e] : 0.f;
-            put4_pair(Es + i * kTok + spread(j0), L::kSquare, x0);
-            // after the rows: in a diagonal tile these places hold its zeros
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, x[e]);
-        }
-    }
-    // what F and F^T have not: half of the steps of 32 tokens on the diagonal
-    if (wave >= 4) {
-        const int t = 2 * (wave & 1);
-        E *to = wave < 6 ? F + (16 * t + col) * kTok + spread(16 * t + 16 + 4 * q) : Ft + (16 * t + 16 + col) * kTok + spread(16 * t + 4 * q);
-        if (wave < 6) put4(to, L::kSquare, zero4());
-        else put4_pair(to, L::kSquare, zero4());
-    }
-    __syncthreads();
-    // dQ += F K, dK += F^T Q + (E + E^T) K
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-        const int p = 32 * kb + 8 * q;
-        const Exact k = get8(Kt + dcol * kTok + p), qq = get8(Qt + dcol * kTok + p);
-#pragma unroll
-        for (int t = 0; t < TI; ++t) {
-            const int ti = ti0 + t;
-            Pair e;
-            get8(Es + (16 * ti + col) * kTok + p, L::kSquare, e);
-            dk[t] = mma(e, k, dk[t]);
-            if (ti >= 2 * kb) {         // F is lower triangular
-                Split f;
-                get8(F + (16 * ti + col) * kTok + p, L::kSquare, f);
-                dq[t] = mma(f, k, dq[t]);
-            }
-            if (ti < 2 * kb + 2) {
-                Pair f;
-                get8(Ft + (16 * ti + col) * kTok + p, L::kSquare, f);
-                dk[t] = mma(f, qq, dk[t]);
+            for (int t = 0; t < TI; t += 2) {
+                store_rows<X>(outq, 16 * (ti0 + t), n, z.dk, d0, dq[t], dq[t + 1], lane);
+                store_rows<X>(outk, 16 * (ti0 + t), n, z.dk, d0, dk[t], dk[t + 1], lane);
             }
         }
-    }
-    {
-        float v[4 * TI];
+        __syncthreads();
+        if (wave == 0) {
+            float mine = -vd[lane], tail = 0.f;
 #pragma unroll
-        for (int t = 0; t < TI; ++t) {
-            float x[4];
-            get4(Qt + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * dq[t][e];
-        }
-        const float s = sum_lanes<TI>(v, lane);
-        const int w = col % (4 * TI);
-        if (col < 4 * TI) qd[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
-    }
-    const int d0 = dcol - col;
-    if (a.shared) {
-        const buffer_t outq = buffer(static_cast<float *>(a.dQ) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
-        const buffer_t outk = buffer(static_cast<float *>(a.dK) + at * C * z.dk, static_cast<size_t>(C) * z.dk);
-#pragma unroll
-        for (int t = 0; t < TI; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int to = state_offset(16 * (ti0 + t) + 4 * q + e, z.dk, dcol);
-                put_buffer(outq, to, dq[t][e]);
-                put_buffer(outk, to, dk[t][e]);
+            for (int w = 0; w < 8; ++w) {
+                mine += qd[w * C + lane];
+                tail += part[w];
             }
-    } else {
-        E *outq = static_cast<E *>(a.dQ) + qk_row(z, bh, t0) * z.dk, *outk = static_cast<E *>(a.dK) + qk_row(z, bh, t0) * z.dk;
+            float s = mine;         // sum over this token and those behind it
 #pragma unroll
-        for (int t = 0; t < TI; t += 2) {
-            store_rows<X>(outq, 16 * (ti0 + t), n, z.dk, d0, dq[t], dq[t + 1], lane);
-            store_rows<X>(outk, 16 * (ti0 + t), n, z.dk, d0, dk[t], dk[t + 1], lane);
+            for (int d = 1; d < 64; d *= 2) {
+                const float y = __shfl_down(s, d);
+                if (lane + d < 64) s += y;
+            }
+            if (lane < n) a.dg[row0 + lane] = s + tail;
         }
-    }
-    __syncthreads();
-    if (wave == 0) {
-        float mine = -vd[lane], tail = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            mine += qd[w * C + lane];
-            tail += part[w];
-        }
-        float s = mine;         // sum over this token and those behind it
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const float y = __shfl_down(s, d);
-            if (lane + d < 64) s += y;
-        }
-        if (lane < n) a.dg[row0 + lane] = s + tail;
     }
 }
 
@@ -1532,8 +1567,9 @@ struct Passes {
             const float *a_S = floats(ws, p.off_S), *a_U = floats(ws, p.off_U);
             const bool shared = p.H != p.Hk;
             GradArgs g{z, io.Q, io.K, io.V, io.dO, r.dec, a_S, a_U, full.dS, full.dR,
-                       shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta};
-            DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3(z.chunks, p.BH), kGradThreads, (GradLds<X, DK>::kBytes), st, g);
+                       shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta,
+                       std::max(1, (z.chunks * p.BH + 255) / 256)};
+            DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3((z.chunks + g.each - 1) / g.each, p.BH), kGradThreads, (GradLds<X, DK>::kBytes), st, g);
             if (shared) {
                 const int rows = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(z.chunks) * C, p.N - static_cast<int64_t>(z.chunk0) * C));
                 const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(rows) * p.dk + 255) / 256), p.BH / p.H * p.Hk);
