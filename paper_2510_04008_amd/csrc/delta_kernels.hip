@@ -379,6 +379,15 @@ __device__ __forceinline__ void keep_rows(float *p, int rows, int row0, int widt
 // dealt to the accumulators so that two of them, as an operand, hold rows 8 q .. 8 q + 7 of 32 (the order of K's rows in memory).
 __device__ __forceinline__ int state_row(int tile, int q, int e) { return 32 * (tile >> 1) + 8 * q + 4 * (tile & 1) + e; }
 __device__ __forceinline__ int state_offset(int row, int dv, int col) { return col < dv ? 4 * (row * dv + col) : kNowhere; }
+// A transition, a DK x DK matrix, lies in the order in which it is read as a left operand: 512 elements together for 16 rows (dealt as above) by 32
+// columns, plane after plane.
+constexpr int kOperand = 512;
+template <class X, int DK>
+__device__ __forceinline__ int transition_place(int row, int k)
+{
+    const int tile = 2 * (row >> 5) + (row >> 2 & 1), m = (row >> 3 & 3) * 4 + (row & 3);
+    return (tile * (DK / 32) + (k >> 5)) * X::kPlanes * kOperand + ((k >> 3 & 3) * 16 + m) * 8 + (k & 7);
+}
 template <int TILES>
 __device__ __forceinline__ void get_state(f32x4 (&S)[TILES], const float *state, int dk, int dv, int tile0, int col, int lane)
 {
@@ -595,18 +604,18 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, DK, 16 * t, z.dvp, 16 * tile, operand<Split>(S[t], S[t + 1]), lane);
     }
     if (trans) {
-        // P as a left operand, row by row; P^T: its columns, of which a lane holds eight rows that lie together
+        // P row by row; P^T: its columns, of which a lane holds eight rows that lie together
         E *P = static_cast<E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
         E *PT = static_cast<E *>(a.PT) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
         const int k0 = 16 * tile - z.dvp;
 #pragma unroll
         for (int t = 0; t < DK / 16; t += 2) {
             const Split x = operand<Split>(S[t], S[t + 1]);
-            put8(PT + (k0 + col) * DK + 16 * t + 8 * q, DK * DK, x);
+            put8(PT + transition_place<X, DK>(k0 + col, 16 * t + 8 * q), kOperand, x);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const f32x4 y = mma(x, unit8<X, false>(b, lane), zero4());
-                put4(P + (16 * t + 16 * b + col) * DK + k0 + 4 * q, DK * DK, y);
+                put4(P + transition_place<X, DK>(16 * t + 16 * b + col, k0 + 4 * q), kOperand, y);
             }
         }
         return;
@@ -637,6 +646,8 @@ struct CombineArgs {
     size_t out_head;
 };
 
+constexpr int kAheadSteps = 2;
+
 template <class X, int DK, int COLS, bool REV>
 __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 {
@@ -656,7 +667,7 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     struct Step {
         Split P[DK / 32];
         f32x4 B[COLS];
-    } ahead[2];
+    } ahead[kAheadSteps];
     f32x4 S[COLS];
 #pragma unroll
     for (int n = 0; n < COLS; ++n) S[n] = zero4();
@@ -670,9 +681,9 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     };
     auto take = [&](int i, Step &to) {
         const size_t s = static_cast<size_t>(bh) * a.p_head + segment(i);
-        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + state_row(wave, lane >> 2 & 3, lane & 3) * DK + 8 * q;
+        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + wave * (DK / 32) * X::kPlanes * kOperand + lane * 8;
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) get8(p + 32 * kb, DK * DK, to.P[kb]);
+        for (int kb = 0; kb < DK / 32; ++kb) get8(p + kb * X::kPlanes * kOperand, kOperand, to.P[kb]);
 #pragma unroll
         for (int n = 0; n < COLS; ++n) to.B[n] = zero4();
         if (!trans) get(to.B, a.add + s * one);
@@ -699,7 +710,7 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
             }
 #pragma unroll
         for (int n = 0; n < COLS; ++n) S[n] = sums[n][0] + sums[n][1];
-        if (i + 2 < end) take(i + 2, my);
+        if (i + kAheadSteps < end) take(i + kAheadSteps, my);
     };
     if (trans) {
 #pragma unroll
@@ -709,12 +720,13 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     } else if (a.carry) {
         get(S, a.carry + bh * a.carry_head + group * a.carry_group);
     }
-    if (begin < end) take(begin, ahead[0]);
-    if (begin + 1 < end) take(begin + 1, ahead[1]);
-    for (int i = begin; i < end; i += 2) {
-        step(i, ahead[0], ops[0]);
-        if (i + 1 < end) step(i + 1, ahead[1], ops[1]);
-    }
+#pragma unroll
+    for (int k = 0; k < kAheadSteps; ++k)
+        if (begin + k < end) take(begin + k, ahead[k]);
+    for (int i = begin; i < end; i += kAheadSteps)
+#pragma unroll
+        for (int k = 0; k < kAheadSteps; ++k)
+            if (i + k < end) step(i + k, ahead[k], ops[(i + k) & 1]);
     if (a.out_P) {
         const size_t g = static_cast<size_t>(bh) * a.out_head + group;
         if (trans) {
@@ -722,7 +734,7 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 #pragma unroll
             for (int n = 0; n < COLS; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) put1(P + state_row(wave, q, e) * DK + col0 + 16 * n - z.dvp, DK * DK, S[n][e]);
+                for (int e = 0; e < 4; ++e) put1(P + transition_place<X, DK>(state_row(wave, q, e), col0 + 16 * n - z.dvp), kOperand, S[n][e]);
         } else {
             put_to(a.out_add + g * one);
         }
