@@ -364,15 +364,25 @@ __device__ __forceinline__ void store_rows(typename X::E *p, int row0, int rows,
         if (row < rows && k < width) store4(p + static_cast<int64_t>(row) * width + k, y);
     }
 }
-// Two accumulators on top of one another, as the operand that they are, into an image of the workspace: 32 rows from row0, columns k0 .. k0 + 15 in
-// spread order.  STATE: rows dealt as the state's.
-template <class X, bool STATE>
-__device__ __forceinline__ void keep_rows(float *p, int rows, int row0, int width, int k0, const typename X::Split &x, int lane)
+// Two accumulators on top of one another, as the operand that they are, into the workspace.  Tokens (U, dR): rows row0 .. + 31 of a 64 x dvp image, columns
+// k0 .. k0 + 15 in spread order.
+template <class X>
+__device__ __forceinline__ void keep_tokens(float *p, int row0, int width, int k0, const typename X::Split &x, int lane)
 {
-    const buffer_t image = buffer(p, static_cast<size_t>(rows) * width);
+    const buffer_t image = buffer(p, static_cast<size_t>(C) * width);
     const int to = 4 * ((lane & 15) * width + spread(k0 + 4 * (lane >> 4)));
 #pragma unroll
-    for (int b = 0; b < 2; ++b) put_buffer(image, to + 4 * (row0 + 16 * b) * width, mma(x, unit8<X, !STATE>(b, lane), zero4()));
+    for (int b = 0; b < 2; ++b) put_buffer(image, to + 4 * (row0 + 16 * b) * width, mma(x, unit8<X, true>(b, lane), zero4()));
+}
+// States: in the order in which they are read as right operands, of dk, 256 floats together (16 rows, half of a step of 32 columns)
+__device__ __forceinline__ int state_place(int tile, int step, int half, int steps) { return ((tile * steps + step) * 2 + half) * 256; }
+template <class X, int DK>
+__device__ __forceinline__ void keep_state(float *p, int tile0, int width, int k0, const typename X::Split &x, int lane)
+{
+    const buffer_t image = buffer(p, static_cast<size_t>(DK) * width);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+        put_buffer(image, 4 * (state_place(tile0 + b, k0 >> 5, k0 >> 4 & 1, width / 32) + 4 * lane), mma(x, unit8<X, false>(b, lane), zero4()));
 }
 
 // A wavefront's 16 columns of a (dk, dv) fp32 state; rows and columns that it has not are zero, and are not written.  Rows are
@@ -533,7 +543,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         for (int kb = 0; kb < DK / 32; ++kb) {
             const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
-            if (MODE == kKeep) keep_rows<X, true>(a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, DK, 32 * kb, z.dvp, 16 * tile, s, lane);
+            if (MODE == kKeep) keep_state<X, DK>(a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, 2 * kb, z.dvp, 16 * tile, s, lane);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
                 R[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, R[ti]);
@@ -581,7 +591,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         if (MODE == kKeep) {
             float *keep = a.U + at * C * z.dvp;
 #pragma unroll
-            for (int ti = 0; ti < 4; ti += 2) keep_rows<X, false>(keep, C, 16 * ti, z.dvp, 16 * tile, operand<Split>(U[ti], U[ti + 1]), lane);
+            for (int ti = 0; ti < 4; ti += 2) keep_tokens<X>(keep, 16 * ti, z.dvp, 16 * tile, operand<Split>(U[ti], U[ti + 1]), lane);
         }
         fence();
         // the state behind the chunk
@@ -601,7 +611,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     if (MODE == kKeep && c1 == z.chunks) {
         float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
 #pragma unroll
-        for (int t = 0; t < DK / 16; t += 2) keep_rows<X, true>(keep, DK, 16 * t, z.dvp, 16 * tile, operand<Split>(S[t], S[t + 1]), lane);
+        for (int t = 0; t < DK / 16; t += 2) keep_state<X, DK>(keep, t, z.dvp, 16 * tile, operand<Split>(S[t], S[t + 1]), lane);
     }
     if (trans) {
         // P row by row; P^T: its columns, of which a lane holds eight rows that lie together
@@ -836,7 +846,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
         for (int kb = 0; kb < DK / 32; ++kb) {
             const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
-            if (FULL) keep_rows<X, true>(a.dS + at * DK * z.dvp, DK, 32 * kb, z.dvp, 16 * tile, s, lane);
+            if (FULL) keep_state<X, DK>(a.dS + at * DK * z.dvp, 2 * kb, z.dvp, 16 * tile, s, lane);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) U[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, U[ti]);
         }
@@ -866,7 +876,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
             E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int ti = 0; ti < 4; ti += 2) {
-                keep_rows<X, false>(keep, C, 16 * ti, z.dvp, 16 * tile, operand<Split>(R[ti], R[ti + 1]), lane);
+                keep_tokens<X>(keep, 16 * ti, z.dvp, 16 * tile, operand<Split>(R[ti], R[ti + 1]), lane);
                 store_rows<X>(dV, 16 * ti, n, z.dv, 16 * tile, strengths(ti) * R[ti], strengths(ti + 1) * R[ti + 1], lane);
             }
         }
@@ -981,7 +991,14 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     auto take_state = [&](const float *from, float (&to)[4][8]) {
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
-            if (kb < deep) kept8(from + dcol * z.dvp + 32 * kb + 8 * q, to[kb]);
+            if (kb < deep) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(from + state_place(dcol >> 4, kb, half, deep) + 4 * lane);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) to[kb][4 * half + e] = x[e];
+                }
+            }
     };
     auto take = [&](int c) {
         const bool has_k = tid < 2 * DK, has_q = tid >= kGradThreads - 2 * DK;
