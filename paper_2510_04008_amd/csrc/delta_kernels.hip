@@ -96,8 +96,7 @@ struct PrepArgs {
     Sizes z;
     const void *Q, *K;
     const float *g, *beta;
-    void *T;                // 64 x 64 images, rows in spread order: T - I (Pairs); backward also M^T and T^T - I (fp32)
-    float *MT, *TT;
+    float *T, *MT, *TT;     // 64 x 64 images, rows in spread order: T - I; backward also M^T and T^T - I
     float *dec;             // per chunk (kDec): e^G, e^{G_C - G}, beta, and G as the sum of two floats
 };
 
@@ -194,7 +193,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
             if (k + e == row) v[e] = 0.f;
             w[e] = k + e == row || !BWD ? 0.f : A[k + e][row];
         }
-        put4_pair(static_cast<E *>(a.T) + at * X::kPairPlanes * C * C + row * C + spread(k), C * C, v);
+        *reinterpret_cast<f32x4 *>(a.T + at * C * C + row * C + spread(k)) = v;
         if (BWD) *reinterpret_cast<f32x4 *>(a.TT + at * C * C + row * C + spread(k)) = w;
     }
 }
@@ -272,28 +271,6 @@ struct ImageStage {
             OPERAND s;
             split8(x[i], s);
             put8(dst + (task >> 3) * kTok + (task & 7) * 8, C * kTok, s);
-        }
-    }
-};
-
-// a 64 x 64 image of Pairs on its way into LDS
-template <int THREADS>
-struct PairStage {
-    static constexpr int kEach = 1024 / THREADS;
-    u32x4 x[kEach];
-    __device__ __forceinline__ void take(const void *src, int tid)
-    {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) x[i] = static_cast<const u32x4 *>(src)[tid + THREADS * i];
-    }
-    template <class X>
-    __device__ __forceinline__ void put(typename X::E *dst, int tid) const
-    {
-        constexpr int kTok = C + X::kPad, kPer = 16 / sizeof(typename X::E);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = (tid + THREADS * i) * kPer;      // planes behind one another: rows of one tile of 64 or 128 rows
-            *reinterpret_cast<u32x4 *>(dst + at / C * kTok + at % C) = x[i];
         }
     }
 };
@@ -425,8 +402,8 @@ enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's tran
 
 struct ScanArgs {
     Sizes z;
-    const void *Q, *K, *V, *T;
-    const float *dec;
+    const void *Q, *K, *V;
+    const float *T, *dec;
     const float *start;             // state at the start of a segment, (dk, dv) fp32: start + bh * start_head + segment * dk * dv; null: zero
     size_t start_head;
     float *final_state;             // state behind the window's last segment (null: not wanted); kPre: behind every segment
@@ -445,7 +422,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     typedef typename X::Pair Pair;
     typedef Lds<X, DK> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPairPlanes * L::kSquare;
+    E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPlanes * L::kSquare;
     E *Ms = Qs + L::kByTokens;
     float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPairPlanes * L::kSquare : Qs);
     const Sizes &z = a.z;
@@ -473,7 +450,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     }
     constexpr bool kAhead = sizeof(E) == 2;         // fp32 operands leave no registers for the images
     RowsStage<X, DK> rows;
-    PairStage<THREADS> is;
+    ImageStage<THREADS> is;
     ColumnsStage<X> vs;
     const typename X::Exact unit = ColumnsStage<X>::unit(z.dv, 16 * tile, lane);
     float ds[(kDec + THREADS - 1) / THREADS];
@@ -483,7 +460,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         const size_t at = static_cast<size_t>(bh) * z.chunks + c;
         if (has_k || has_q) rows.take(static_cast<const E *>(has_k ? a.K : a.Q) + qk_row(z, bh, t0) * z.dk, n, z.dk, task);
         if (kAhead) {
-            is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
+            is.take(a.T + at * C * C, tid);
         }
 #pragma unroll
         for (int i = 0; i < (kDec + THREADS - 1) / THREADS; ++i)
@@ -508,8 +485,8 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         __syncthreads();
         if (has_k) rows.template put<true, true>(n, z.dk, Ks, Kt, task);
         if (has_q) rows.template put<true, false>(n, z.dk, Qs, nullptr, task);
-        if (!kAhead) is.take(static_cast<const E *>(a.T) + at * X::kPairPlanes * C * C, tid);
-        is.template put<X>(Ts, tid);
+        if (!kAhead) is.take(a.T + at * C * C, tid);
+        is.template put<X, Split>(Ts, tid);
 #pragma unroll
         for (int i = 0; i < (kDec + THREADS - 1) / THREADS; ++i)
             if (tid + THREADS * i < kDec) dec[tid + THREADS * i] = ds[i];
@@ -571,10 +548,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         for (int ti = 0; ti < 4; ++ti) U[ti] = R[ti];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const Pair r = operand<Pair>(R[2 * kb], R[2 * kb + 1]);
+            const Split r = operand<Split>(R[2 * kb], R[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
 #pragma unroll
-            for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Pair, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
+            for (int ti = 2 * kb; ti < 4; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), r, U[ti]);
         }
         if (MODE == kOut) {
             __syncthreads();
@@ -1352,7 +1329,7 @@ template <class X, int DK>
 constexpr size_t scan_lds(bool out)
 {
     typedef Lds<X, DK> L;
-    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPairPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + kDec * sizeof(float);
+    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + kDec * sizeof(float);
 }
 template <class X, int DK>
 constexpr size_t rev_lds()
@@ -1397,7 +1374,7 @@ struct Passes {
     static constexpr int kTiles = THREADS / 64;
     static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
     {
-        PrepArgs a{z, io.Q, io.K, io.g, io.beta, ws + p.off_T, bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
+        PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
         const dim3 grid(z.chunks, p.BH);
         if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
         else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
@@ -1410,7 +1387,7 @@ struct Passes {
         a.Q = io.Q;
         a.K = io.K;
         a.V = io.V;
-        a.T = ws + p.off_T;
+        a.T = floats(ws, p.off_T);
         a.dec = floats(ws, p.off_dec);
         return a;
     }
