@@ -341,8 +341,13 @@ race_status_t race_qk_rotary_bwd(const race_rotary_desc_t *desc, const void *q, 
     race_status_t s = plan_rotary(desc, &p);
     if (s != RACE_OK) return s;
     const bool keys = p.k.heads > 0;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (rows_overlap(desc, desc->Hq, desc->dq_strides) || (keys && rows_overlap(desc, desc->Hk, desc->dk_strides))) return RACE_ERR_INVALID_ARG;
-    if (p.N == 0) return RACE_OK;           // nothing to do, pointers may be null
+    if (p.N == 0) {                         // no rows, other pointers may be null; the sums over them are zero
+        hipError_t e = dwq ? zero_floats(dwq, p.d, st) : hipSuccess;
+        if (e == hipSuccess && dwk && keys) e = zero_floats(dwk, p.d, st);
+        return e == hipSuccess ? RACE_OK : hip_failed(e, "race_qk_rotary_bwd launch");
+    }
     if (!q || !dQ || !dq || (keys && (!k || !dK || !dk)) || (!keys && dwk)) return RACE_ERR_INVALID_ARG;
     if ((s = read_turns(desc, inv_freq, &p)) != RACE_OK) return s;
     if (any_equal({dq}, {q, k, wq, wk, positions, dQ, dK, dq, dk, dwq, dwk}) || (keys && any_equal({dk}, {q, k, wq, wk, positions, dQ, dK, dq, dk, dwq, dwk})))
@@ -354,7 +359,7 @@ race_status_t race_qk_rotary_bwd(const race_rotary_desc_t *desc, const void *q, 
     p.positions = positions;
     p.q.x = q, p.q.w = wq, p.q.y = const_cast<void *>(dQ), p.q.dx = dq;
     p.k.x = k, p.k.w = wk, p.k.y = const_cast<void *>(dK), p.k.dx = dk;
-    hipError_t e = rotary::backward(p, dwq, dwk, static_cast<char *>(workspace), reinterpret_cast<hipStream_t>(stream));
+    hipError_t e = rotary::backward(p, dwq, dwk, static_cast<char *>(workspace), st);
     return e == hipSuccess ? RACE_OK : hip_failed(e, "race_qk_rotary_bwd launch");
 }
 

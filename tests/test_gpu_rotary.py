@@ -156,6 +156,16 @@ def test_special_rows():
                     assert torch.equal(got[a][0, h, n], want[b][0, h, n])
 
 
+def test_no_tokens():
+    x = {n: v.cuda() for n, v in _inputs(2, 0, 2, 1, 32, "bf16").items()}
+    desc = ra.make_rotary_desc(2, 0, 2, 1, 32, 32, ra.RACE_BF16)
+    Q, K = ra.race_qk_rotary_fwd(desc, x["q"], x["k"], x["wq"], x["wk"], _freq(32))
+    dwq, dwk = (torch.full((32,), 7.0, device="cuda") for _ in range(2))
+    dq, dk, _, _ = ra.race_qk_rotary_bwd(desc, x["q"], x["k"], x["wq"], x["wk"], _freq(32), None, x["dQ"], x["dK"], dwq=dwq, dwk=dwk)
+    assert Q.shape == (2, 2, 0, 32) and K.shape == (2, 1, 0, 32) and dq.shape == (2, 0, 2, 32) and dk.shape == (2, 0, 1, 32)
+    assert (dwq == 0).all() and (dwk == 0).all()
+
+
 def test_streams_and_graphs():
     x = _inputs(2, 40, 4, 2, 128, "bf16")
     desc = ra.make_rotary_desc(2, 40, 4, 2, 128, 128, ra.RACE_BF16)
