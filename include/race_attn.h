@@ -227,16 +227,17 @@ race_status_t race_attn_step(const race_attn_desc_t *desc, const void *q, const 
  *   - g is the logarithm of the decay, usually <= 0; -infinity (every value below -1e5) empties the state before the token is written.  beta is
  *     used as given.  Rows of Q and K are used as given: a bounded state wants |k| <= 1 with beta in [0, 2] (race_qk_rotary_fwd makes such rows).
  *   - A padding token is one with g = 0 and beta = 0: the state passes it unchanged; its rows must be finite.
- *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64).  The bf16 type multiplies states and
- *     their cotangents as the sum of two bf16; O, dQ, dK and dV are rounded to bf16 at the end.
+ *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64; a sum over part of 64 tokens has to stay
+ *     below 88, where exp leaves fp32).  The bf16 type multiplies fp32 values as sums of three bf16, all 24 bits (of two where only a bf16 output depends
+ *     on the product); O, dQ, dK and dV are rounded to bf16 at the end.
  *   - A non-finite element of Q, K, V or dO reaches what depends on it, and may spread over the 64 tokens of its chunk, for bf16 and
  *     fp32 alike; it does not reach another head or sequence (Q, K: other than those that share them).
  *   - Pointers need be aligned to their elements only.  Buffers must not overlap, except that a state may be carried in place: state_out
  *     may be state_in, dstate_in may be dstate_out.
  *   - Everything else (workspace, streams, errors, capture into a graph) as above.  Results are the same bits every time. */
 typedef struct {
-    int32_t B, H, Hk; /* batch, value heads, heads of queries and keys (H a multiple of Hk)             */
-    int64_t N;        /* tokens per sequence (>= 0)                                                     */
+    int32_t B, H, Hk; /* batch, value heads, heads of queries and keys (H a multiple of Hk); B * H up to 65535 */
+    int64_t N;        /* tokens per sequence (>= 0); B * H * N up to 2^36                               */
     int32_t dk, dv;   /* multiples of 8, 8 .. 128.  (A wider value row: two value heads of half of it, with the same g, beta and shared q, k) */
     float scale;      /* of the outputs, finite                                                         */
     int32_t dtype;    /* race_dtype_t                                                                   */
@@ -279,8 +280,8 @@ race_status_t race_delta_step(const race_delta_desc_t *desc, const void *q, cons
  *   - Arithmetic is fp32, rounded once to desc->dtype.  A non-finite element spreads over its own row.  Pointers need be aligned to their elements only. */
 typedef enum { RACE_NORM_NONE = 0, RACE_NORM_RMS = 1, RACE_NORM_L2 = 2 } race_norm_t;
 typedef struct {
-    int32_t B, Hq, Hk;     /* batch, heads of queries (>= 1) and keys (>= 0)                                  */
-    int64_t N;             /* tokens per sequence (>= 0)                                                      */
+    int32_t B, Hq, Hk;     /* batch, heads of queries (>= 1) and keys (>= 0), Hq + Hk up to 65535             */
+    int64_t N;             /* tokens per sequence (>= 0); B * N up to 2^31                                    */
     int32_t d, rot;        /* row: multiple of 8, 8 .. 256; rotated elements: even, 0 .. d                    */
     int32_t norm;          /* race_norm_t                                                                     */
     int32_t neighbours;    /* 0: pairs (i, i + rot/2), 1: pairs (2i, 2i + 1)                                  */

@@ -15,7 +15,7 @@ using delta::kJoinInGroups;
 
 constexpr int kChunk = 64;
 constexpr int kMaxHeads = 65535;            // B H: a grid dimension
-constexpr int64_t kMaxTokens = int64_t(1) << 36;
+constexpr int64_t kMaxTokens = int64_t(1) << 36;       // of all sequences and heads (rows of queries and keys: of a sequence)
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
@@ -33,8 +33,9 @@ race_status_t check_delta(const race_delta_desc_t *d)
 {
     if (!d || d->B < 1 || d->H < 1 || d->Hk < 1 || d->N < 0 || d->dk < 1 || d->dv < 1 || d->chunk < 0 || !std::isfinite(d->scale)) return RACE_ERR_INVALID_ARG;
     if ((d->dtype != RACE_F32 && d->dtype != RACE_BF16) || d->H % d->Hk != 0) return RACE_ERR_INVALID_ARG;
-    if (d->dk % 8 || d->dv % 8 || d->dk > 128 || d->dv > 128 || d->N > kMaxTokens) return RACE_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(d->B) * d->H > kMaxHeads) return RACE_ERR_UNSUPPORTED;
+    if (d->dk % 8 || d->dv % 8 || d->dk > 128 || d->dv > 128) return RACE_ERR_UNSUPPORTED;
+    const int64_t heads = static_cast<int64_t>(d->B) * d->H;
+    if (heads > kMaxHeads || d->N > kMaxTokens / heads) return RACE_ERR_UNSUPPORTED;
     return RACE_OK;
 }
 
@@ -80,7 +81,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     const size_t per_chunk = square * 4 + 5 * kChunk * 4 + (backward ? square * 8 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
     const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
-        p.seg_chunks = static_cast<int>(std::min<int64_t>((d->chunk + kChunk - 1) / kChunk, p.chunks));
+        p.seg_chunks = static_cast<int>((std::min(d->chunk, d->N) + kChunk - 1) / kChunk);
         p.win_segs = std::max(1, window < p.chunks ? window / p.seg_chunks : (p.chunks + p.seg_chunks - 1) / p.seg_chunks);
     } else {
         p.win_segs = choose_segments(window, p.BH);

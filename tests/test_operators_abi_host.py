@@ -84,6 +84,21 @@ def test_delta_segments_cover_the_sequence(B, H, N):
         assert ra.race_delta_segment_tokens(d) == min(-(-chunk // 64), -(-N // 64)) * 64
 
 
+@pytest.mark.parametrize("chunk", [(1 << 63) - 1, (1 << 63) - 64, 1 << 40])
+def test_delta_segment_longer_than_any_sequence(chunk):
+    for N in (1, 1000, 1 << 20):
+        d, whole = _delta(N=N, chunk=chunk), _delta(N=N, chunk=N)
+        assert ra.race_delta_segment_tokens(d) == -(-N // 64) * 64
+        assert ra.race_delta_workspace_bytes(d) == ra.race_delta_workspace_bytes(whole) > 0
+        assert ra.race_delta_bwd_workspace_bytes(d) == ra.race_delta_bwd_workspace_bytes(whole) > 0
+
+
+def test_delta_refuses_more_tokens_than_bytes_can_be_counted():
+    assert ra.race_delta_bwd_workspace_bytes(_delta(B=1, H=4, N=1 << 34, chunk=64)) > 0
+    for bad in (dict(B=65535, H=1, Hk=1, N=1 << 36), dict(B=1, H=4, N=(1 << 34) + 1)):
+        assert ra.race_delta_bwd_workspace_bytes(_delta(**bad)) == 0 and _fwd(_delta(**bad)) == ra.RACE_ERR_UNSUPPORTED
+
+
 def test_delta_workspace_is_bounded():
     # beyond the first window only what a segment leaves behind grows
     one, two = (ra.race_delta_bwd_workspace_bytes(_delta(B=1, H=4, N=n, dk=128, dv=128)) for n in (1 << 22, 1 << 23))
