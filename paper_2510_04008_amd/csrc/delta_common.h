@@ -48,13 +48,12 @@ constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 
 // l % 16 and, with q = l / 16, eight of the 32 k: 8 q + 0..7 ("natural") or 16 a + 4 q + r, a = 0, 1, r = 0..3 ("spread": the rows of two
 // accumulators that lie on top of one another, so that a product's result is the next product's operand without leaving the registers).  Any
 // order will do, as long as both operands have it; tiles and images whose rows run over tokens or over columns of the state are stored in spread order.
-// The kernels that are parallel over chunks multiply 32 x 32 tiles, 16 deep, half as many operands to a product: lane l holds row l % 32
-// and the eight places 8 h + 0..7, h = l / 32, of the stored order.
+// K K^T and Q K^T of prep are 32 x 32 tiles, 16 deep, half as many operands to a product: lane l holds row l % 32 and the elements 8 h + 0..7, h = l / 32.
 //
 // bf16: the elements of Q, K, V and dO are exact as they are.  Values that are fp32 by their nature enter as
 // sums of bf16: three (Split: all 24 bits) where fp32 outputs (state, dg, db) hang on them, two (Pair: off by at most 2^-16) where
-// outputs of the element type alone do.  One bf16 (2^-8) would leave the fp32 outputs three digits; with two of them throughout dg was 1.5e-5 off at dk = 16.
-// The matrix instructions of the additional products are not what bounds any of the kernels.
+// outputs of the element type alone do.  One bf16 (2^-8) would leave the fp32 outputs three digits; with two of them throughout dg was 1.5e-5 off at dk = 16,
+// with three it and the states are within 5e-7 of a computation in 64 bits.  T as a Split and not a Pair costs the passes 7 to 15 % of their time.
 // fp32: eight fp32 matrix instructions a product, one for each of a lane's k.
 struct Bf {
     typedef uint16_t E;

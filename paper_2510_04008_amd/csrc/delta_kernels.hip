@@ -42,21 +42,15 @@ __device__ __forceinline__ void kept8(const float *p, float *x)
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
 }
-template <class OPERAND>
-__device__ __forceinline__ OPERAND kept(const float *p)
-{
-    float x[8];
-    OPERAND s;
-    kept8(p, x);
-    split8(x, s);
-    return s;
-}
 
 // ------------------------------------------------------------------ what a chunk needs besides the states
 // T and the decays of one chunk of one head, and for the backward pass M^T.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane
 // per column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions, each block in A's place.  Substitution and not powers of A: with keys
 // alike the powers reach thousands where T stays near one.
-// Images are written in the order in which the scans' operands lie in LDS (rows in spread order).
+// Images are written in the order in which the scans' operands lie in LDS (rows in spread order), in fp32: half of the bytes of a Split.
+// One workgroup of four wavefronts per chunk and head, several on a CU, so that one's substitution (16 steps of one wavefront) runs beside another's loads.  65536 chunks
+// of dk = 128, bf16 (2^20 tokens, four heads): 686 us, 34 KB a chunk and 3.3 TB/s; wavefronts wait 70 % of their time, for loads and
+// at the barriers between the steps.
 template <int SIZE>
 struct MergeBlocks {
     static constexpr int NT = SIZE / 16;
@@ -398,6 +392,12 @@ __device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state,
 // One workgroup per segment, head and up to eight (four) tiles of 16 columns of the state; a wavefront keeps its columns of the state in
 // accumulators from chunk to chunk (DK x 16 fp32), where they are at once the right operand of the products with K and Q.
 // Columns never meet, so wavefronts share the tiles in LDS and nothing else.
+//
+// What bounds it is the issue of instructions: at dk = dv = 128, bf16, the matrix units are busy 40 to 47 % of the time and the vector ALU, which splits states,
+// R and U into bf16 for the next product, 48 to 58 % (the issue of matrix instructions included); the state's columns in registers (up to 252 a lane) leave room for two wavefronts a SIMD.  Sixteen columns a
+// wavefront and eight wavefronts beat 32 columns and four (one wavefront a SIMD: nothing to fill its waits).  Tried without gain: operands asked for before
+// the split of the state, and priorities for the matrix phases or for half of the wavefronts.  2^20 tokens, four heads, 64 segments, so a workgroup
+// on every CU: 1.90 ms, 7.4 us a chunk; the pre-pass, two workgroups a segment: 2.28 ms; kKeep, 96 KB a chunk more to write, takes 7.4 us a chunk too.
 enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's transition and state from zero; states and U for the backward pass
 
 struct ScanArgs {
@@ -616,6 +616,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 // wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
 // asked for two steps ahead.  A step takes 2 to 3 us all the same, most of it P on its way, so many segments are joined in groups of about the root of
 // their number: the transitions of the groups side by side (compose), the groups one after the other, then the segments of all groups side by side.
+// 63 transitions of four heads, dk = dv = 128, bf16: 66 us in the three launches, about 190 one after the other.
 struct CombineArgs {
     Sizes z;
     int heads, groups, each;        // transitions of a group: each; the last group's may be fewer
@@ -731,6 +732,8 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 }
 
 // ------------------------------------------------------------------ cotangents of the states, last chunk first
+// The scan's mirror image: the same split of the work, the same bound (matrix units busy 31 to 36 %, vector ALU 35 to 42 %, two wavefronts a SIMD, and more to
+// stage and to write), 11.7 us a chunk with dV and what the gradients read (FULL: 96 KB a chunk), 8.5 us without, at dk = dv = 128, bf16.
 struct RevArgs {
     Sizes z;
     const void *Q, *K, *dO;
@@ -922,7 +925,10 @@ __device__ __forceinline__ float sum_lanes(float (&v)[4 * TI], int lane)
 
 // One workgroup of eight wavefronts per chunk.  U, dR and dO are read once, into LDS, as operands; a wavefront then has 16 columns of dQ and dK
 // (and with dk <= 64 half of the tokens), for which it reads its rows of S and dS once, as right operands: dO S^T, dR S^T and U dS^T.  F and E are
-// formed from the same tiles before these are overwritten with F, F^T and E + E^T, whose products with K and Q end the kernel.
+// formed from the same tiles before these are overwritten with F, F^T and E + E^T, whose products with K and Q end the kernel.  A workgroup goes on to the
+// chunk before it, whose states it has asked for by then; <S', dS> takes S' from the chunk behind.
+// 4096 chunks of dk = dv = 128, bf16: 382 us for 288 KB a chunk, 3.1 TB/s.  LDS holds one workgroup of a CU, which waits for its own reading: wavefronts wait 43 % of
+// their time (matrix units busy 14 %, vector ALU 42 %).
 constexpr int kGradThreads = 512;
 
 template <class X, int DK>
@@ -1269,7 +1275,9 @@ __global__ __launch_bounds__(256) void delta_shared_heads_kernel(Sizes z, int ro
 
 // ------------------------------------------------------------------ one token
 // The state is read and written once and everything else is small.  A workgroup owns 32 columns of one head's state: 8 lanes of four
-// columns by 32 groups of rows, four rows a lane (dk = 128), all held in registers between the two sums over rows.
+// columns by 32 groups of rows, four rows a lane (dk = 128), all held in registers between the two sums over rows.  Memory bounds it: 2048 states of
+// 128 x 128 (268 MB read and written) take 45 us, 5.9 TB/s, above the 4.9 TB/s of a copy of 2 GiB because part of the states stays in the last-level cache.
+// Four states take 4 us, which is one launch.
 template <class E>
 __global__ __launch_bounds__(256) void delta_step_kernel(Sizes z, const E *q, const E *k, const E *v, const float *g, const float *beta, float *state, E *o)
 {

@@ -40,16 +40,16 @@ race_status_t check_delta(const race_delta_desc_t *d)
 }
 
 // Segments that run side by side, by the time of a forward pass, in us, from sweeps at dk = dv = 128 (bf16; the other shapes have their minimum
-// in the same places): a chunk takes 6.5 in the pass proper, with a workgroup per segment and head, and 4.2 in the pre-pass, with two; the CUs hold
-// 256 workgroups at once; the join takes 3 a segment one after the other, in groups 25 + 0.7 a segment.  At B H = 4 and 1024 chunks: 64 segments 1845 (training
-// step), 61: 1866, 52: 1965, 43: 2082, 74 (a second round): 2300, 32: 2166.
+// in the same places): a chunk takes 7.2 in the pass proper, with a workgroup per segment and head, and 4.4 in the pre-pass, with two; the CUs hold
+// 256 workgroups at once; the join takes 3 a segment one after the other, in groups 25 + 0.7 a segment.  At B H = 4 and 1024 chunks, training: 64 segments
+// 1521, 61: 1556, 52: 1660, 43: 1807, 32: 1895, 74 (a second round): 1931.
 int choose_segments(int chunks, int BH)
 {
     int best = 1;
-    double cost = 6.5 * chunks;
+    double cost = 7.2 * chunks;
     for (int n = 2; n <= 256 / BH && n <= chunks; ++n) {
         const int m = (chunks + n - 1) / n, rounds = (2 * (n - 1) * BH + 255) / 256;
-        const double c = (6.5 + 4.2 * rounds) * m + (n <= kJoinInGroups ? 3.0 * n : 25.0 + 0.7 * n) + 12.0;
+        const double c = (7.2 + 4.4 * rounds) * m + (n <= kJoinInGroups ? 3.0 * n : 25.0 + 0.7 * n) + 12.0;
         if (c < cost) {
             cost = c;
             best = n;
