@@ -903,23 +903,28 @@ __device__ __forceinline__ typename X::Exact rows8_spread(const typename X::E *t
     const int k = (p & ~31) + ((p & 31) >> 1);
     return load8_spread(t + static_cast<int64_t>(row) * width + k, row < rows && k < width, row < rows && k + 16 < width);
 }
-// sums over 16 lanes of 4 TI values a lane: afterwards lane l holds the sum of value l % (4 TI)
-template <int TI>
-__device__ __forceinline__ float sum_lanes(float (&v)[4 * TI], int lane)
+// Sums over 16 lanes of N values a lane: afterwards lane l holds the sum of value l % N.  M lanes apart, half of the values are handed over at a time.  (A template
+// and not a loop over M: the compiler left such a loop standing and chose each value by sixteen comparisons, half of the kernel's instructions.)
+template <int M, int N>
+__device__ __forceinline__ void fold_lanes(float (&v)[N], int lane)
 {
+    if constexpr (M >= N) {
 #pragma unroll
-    for (int m = 8; m >= 4 * TI; m /= 2)
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], M);
+    } else {
+        const bool up = lane & M;
 #pragma unroll
-        for (int k = 0; k < 4 * TI; ++k) v[k] += __shfl_xor(v[k], m);
-#pragma unroll
-    for (int m = 2 * TI; m >= 1; m /= 2) {
-        const bool up = lane & m;
-#pragma unroll
-        for (int k = 0; k < m; ++k) {
-            const float keep = up ? v[k + m] : v[k], give = up ? v[k] : v[k + m];
-            v[k] = keep + __shfl_xor(give, m);
+        for (int k = 0; k < M; ++k) {
+            const float keep = up ? v[k + M] : v[k], give = up ? v[k] : v[k + M];
+            v[k] = keep + __shfl_xor(give, M);
         }
     }
+    if constexpr (M > 1) fold_lanes<M / 2>(v, lane);
+}
+template <int N>
+__device__ __forceinline__ float sum_lanes(float (&v)[N], int lane)
+{
+    fold_lanes<8>(v, lane);
     return v[0];
 }
 
@@ -1209,7 +1214,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * dq[t][e];
             }
-            const float s = sum_lanes<TI>(v, lane);
+            const float s = sum_lanes(v, lane);
             const int w = col % (4 * TI);
             if (col < 4 * TI) qd[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
         }
