@@ -970,7 +970,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     const float *S0 = a.S + static_cast<size_t>(bh) * (z.chunks + 1) * DK * z.dvp;
     const int deep = z.dvp / 32;            // steps of a product over the state's columns
     int dcol = 16 * (wave % (DK / 16)) + col;
-    const int ti0 = wave / (DK / 16) * TI;
+    const int ti0 = DK == 128 ? 0 : wave / (DK / 16) * TI;
+    constexpr bool kNext = DK == 128;       // a tile's operands are asked for while the one before is multiplied; with dk <= 64 there are only two, and branches
 
     // what a chunk reads: asked for at once, and while the products of the chunk before are formed
     RowsStage<X, DK> rows;
@@ -1111,16 +1112,24 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
             Pair ds;
             split8(s[kb], ss);
             split8(d[kb], ds);
+            Pair u[2], r[2];
+            Exact o[2];
+            auto get = [&](int t) {
+                const int row = 16 * (ti0 + t);
+                get8(Us + (row + col) * kWide + p + 8 * q, C * kWide, u[t & 1]);
+                get8(Rs + (row + col) * kWide + p + 8 * q, C * kWide, r[t & 1]);
+                o[t & 1] = tokens_o(row, p);
+            };
+            if (kNext) get(0);
 #pragma unroll
             for (int t = 0; t < TI; ++t) {
-                const int row = 16 * (ti0 + t);
+                if (!kNext) get(t);
+                else if (t + 1 < TI) get(t + 1);
                 fence();
-                Pair u, r;
-                get8(Us + (row + col) * kWide + p + 8 * q, C * kWide, u);
-                get8(Rs + (row + col) * kWide + p + 8 * q, C * kWide, r);
-                dq[t] = mma(tokens_o(row, p), ss, dq[t]);
-                y[t] = mma(r, lead(ss), y[t]);
-                dk[t] = mma(u, ds, dk[t]);
+                dq[t] = mma(o[t & 1], ss, dq[t]);
+                y[t] = mma(r[t & 1], lead(ss), y[t]);
+                dk[t] = mma(u[t & 1], ds, dk[t]);
+                if (kNext) fence();
             }
         }
 #pragma unroll
@@ -1187,22 +1196,25 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         for (int kb = 0; kb < 2; ++kb) {
             const int p = 32 * kb + 8 * q;
             const Exact k = get8(Kt + dcol * kTok + p), qq = get8(Qt + dcol * kTok + p);
+            Pair e[2], ft[2];
+            Split f[2];
+            auto get = [&](int t) {
+                const int ti = ti0 + t, place = (16 * ti + col) * kTok + p;
+                get8(Es + place, L::kSquare, e[t & 1]);
+                if (ti >= 2 * kb) get8(F + place, L::kSquare, f[t & 1]);           // F is lower triangular
+                if (ti < 2 * kb + 2) get8(Ft + place, L::kSquare, ft[t & 1]);
+            };
+            if (kNext) get(0);
 #pragma unroll
             for (int t = 0; t < TI; ++t) {
                 const int ti = ti0 + t;
-                Pair e;
-                get8(Es + (16 * ti + col) * kTok + p, L::kSquare, e);
-                dk[t] = mma(e, k, dk[t]);
-                if (ti >= 2 * kb) {         // F is lower triangular
-                    Split f;
-                    get8(F + (16 * ti + col) * kTok + p, L::kSquare, f);
-                    dq[t] = mma(f, k, dq[t]);
-                }
-                if (ti < 2 * kb + 2) {
-                    Pair f;
-                    get8(Ft + (16 * ti + col) * kTok + p, L::kSquare, f);
-                    dk[t] = mma(f, qq, dk[t]);
-                }
+                if (!kNext) get(t);
+                else if (t + 1 < TI) get(t + 1);
+                if (kNext) fence();
+                dk[t] = mma(e[t & 1], k, dk[t]);
+                if (ti >= 2 * kb) dq[t] = mma(f[t & 1], k, dq[t]);
+                if (ti < 2 * kb + 2) dk[t] = mma(ft[t & 1], qq, dk[t]);
+                if (kNext) fence();
             }
         }
         {
