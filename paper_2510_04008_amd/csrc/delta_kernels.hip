@@ -360,14 +360,14 @@ __device__ __forceinline__ void keep_state(float *p, int tile0, int width, int k
 // dealt to the accumulators so that two of them, as an operand, hold rows 8 q .. 8 q + 7 of 32 (the order of K's rows in memory).
 __device__ __forceinline__ int state_row(int tile, int q, int e) { return 32 * (tile >> 1) + 8 * q + 4 * (tile & 1) + e; }
 __device__ __forceinline__ int state_offset(int row, int dv, int col) { return col < dv ? 4 * (row * dv + col) : kNowhere; }
-// A transition, a DK x DK matrix, lies in the order in which it is read as a left operand: 512 elements together for 16 rows (dealt as above) by 32
-// columns, plane after plane.
+// A transition, a DK x DK fp32 matrix, lies in the order in which it is read as a left operand: 512 values together for 16 rows (dealt as above) by 32
+// columns.
 constexpr int kOperand = 512;
-template <class X, int DK>
+template <int DK>
 __device__ __forceinline__ int transition_place(int row, int k)
 {
     const int tile = 2 * (row >> 5) + (row >> 2 & 1), m = (row >> 3 & 3) * 4 + (row & 3);
-    return (tile * (DK / 32) + (k >> 5)) * X::kPlanes * kOperand + ((k >> 3 & 3) * 16 + m) * 8 + (k & 7);
+    return (tile * (DK / 32) + (k >> 5)) * kOperand + ((k >> 3 & 3) * 16 + m) * 8 + (k & 7);
 }
 template <int TILES>
 __device__ __forceinline__ void get_state(f32x4 (&S)[TILES], const float *state, int dk, int dv, int tile0, int col, int lane)
@@ -409,7 +409,7 @@ struct ScanArgs {
     float *final_state;             // state behind the window's last segment (null: not wanted); kPre: behind every segment
     size_t final_head;
     void *O;
-    void *P, *PT;                   // kPre: the transition and its transpose (Splits), per segment
+    float *P, *PT;                  // kPre: the transition and its transpose, per segment
     int transitions;                // kPre
     float *S, *U;                   // kKeep: states at the chunks' starts and behind the last, and U, rows in spread order
 };
@@ -592,18 +592,17 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     }
     if (trans) {
         // P row by row; P^T: its columns, of which a lane holds eight rows that lie together
-        E *P = static_cast<E *>(a.P) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
-        E *PT = static_cast<E *>(a.PT) + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * X::kPlanes * DK * DK;
+        float *P = a.P + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK, *PT = a.PT + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK;
         const int k0 = 16 * tile - z.dvp;
 #pragma unroll
         for (int t = 0; t < DK / 16; t += 2) {
             const Split x = operand<Split>(S[t], S[t + 1]);
-            put8(PT + transition_place<X, DK>(k0 + col, 16 * t + 8 * q), kOperand, x);
+            f32x4 *to = reinterpret_cast<f32x4 *>(PT + transition_place<DK>(k0 + col, 16 * t + 8 * q));
+            to[0] = S[t];
+            to[1] = S[t + 1];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const f32x4 y = mma(x, unit8<X, false>(b, lane), zero4());
-                put4(P + transition_place<X, DK>(16 * t + 16 * b + col, k0 + 4 * q), kOperand, y);
-            }
+            for (int b = 0; b < 2; ++b)
+                *reinterpret_cast<f32x4 *>(P + transition_place<DK>(16 * t + 16 * b + col, k0 + 4 * q)) = mma(x, unit8<X, false>(b, lane), zero4());
         }
         return;
     }
@@ -614,22 +613,22 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 // ------------------------------------------------------------------ states at the segments' starts
 // S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 COLS columns, a
 // wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
-// asked for two steps ahead.  A step takes 2 to 3 us all the same, most of it P on its way, so many segments are joined in groups of about the root of
+// asked for two steps ahead (three: no faster).  A step takes 1.5 us all the same, a chain of LDS, barrier and products one after the other, so many segments are joined in groups of about the root of
 // their number: the transitions of the groups side by side (compose), the groups one after the other, then the segments of all groups side by side.
-// 63 transitions of four heads, dk = dv = 128, bf16: 66 us in the three launches, about 190 one after the other.
+// 63 transitions of four heads, dk = dv = 128, bf16: 66 us in the three launches, about 100 one after the other.
 struct CombineArgs {
     Sizes z;
     int heads, groups, each;        // transitions of a group: each; the last group's may be fewer
     int steps;                      // transitions in all: segments first, first + 1, .. (REV: first, first - 1, ..)
     int first;
-    const void *P;                  // P_s: image bh * p_head + s; B_s: add + (bh * p_head + s) * dk * dv
+    const float *P;                 // P_s: image bh * p_head + s; B_s: add + (bh * p_head + s) * dk * dv
     size_t p_head;
     const float *add;
     const float *carry;             // state to start from (null: zero): carry + bh * carry_head + group * carry_group
     size_t carry_head, carry_group;
     float *at;                      // states at the segments' starts (REV: cotangents at their ends): at + bh * at_head + s * dk * dv; null: not wanted
     size_t at_head;
-    void *out_P;                    // compose: the groups' transitions and states from zero, image bh * out_head + group
+    float *out_P;                   // compose: the groups' transitions and states from zero, image bh * out_head + group
     float *out_add;
     size_t out_head;
 };
@@ -653,7 +652,7 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     const size_t one = static_cast<size_t>(z.dk) * z.dv;
     auto segment = [&](int i) { return REV ? a.first - i : a.first + i; };
     struct Step {
-        Split P[DK / 32];
+        float P[DK / 32][8];
         f32x4 B[COLS];
     } ahead[kAheadSteps];
     f32x4 S[COLS];
@@ -669,9 +668,9 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     };
     auto take = [&](int i, Step &to) {
         const size_t s = static_cast<size_t>(bh) * a.p_head + segment(i);
-        const E *p = static_cast<const E *>(a.P) + s * X::kPlanes * DK * DK + wave * (DK / 32) * X::kPlanes * kOperand + lane * 8;
+        const float *p = a.P + s * DK * DK + wave * (DK / 32) * kOperand + lane * 8;
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) get8(p + kb * X::kPlanes * kOperand, kOperand, to.P[kb]);
+        for (int kb = 0; kb < DK / 32; ++kb) kept8(p + kb * kOperand, to.P[kb]);
 #pragma unroll
         for (int n = 0; n < COLS; ++n) to.B[n] = zero4();
         if (!trans) get(to.B, a.add + s * one);
@@ -687,6 +686,9 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
         f32x4 sums[COLS][2];
 #pragma unroll
         for (int n = 0; n < COLS; ++n) sums[n][0] = my.B[n], sums[n][1] = zero4();
+        Split P[DK / 32];
+#pragma unroll
+        for (int kb = 0; kb < DK / 32; ++kb) split8(my.P[kb], P[kb]);
         __syncthreads();
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb)
@@ -694,7 +696,7 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
             for (int n = 0; n < COLS; ++n) {
                 Split s;
                 get8(&op[n][0][kb][lane * 8], DK / 32 * 64 * 8, s);
-                sums[n][kb & 1] = mma(my.P[kb], s, sums[n][kb & 1]);
+                sums[n][kb & 1] = mma(P[kb], s, sums[n][kb & 1]);
             }
 #pragma unroll
         for (int n = 0; n < COLS; ++n) S[n] = sums[n][0] + sums[n][1];
@@ -718,11 +720,11 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
     if (a.out_P) {
         const size_t g = static_cast<size_t>(bh) * a.out_head + group;
         if (trans) {
-            E *P = static_cast<E *>(a.out_P) + g * X::kPlanes * DK * DK;
+            float *P = a.out_P + g * DK * DK;
 #pragma unroll
             for (int n = 0; n < COLS; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) put1(P + transition_place<X, DK>(state_row(wave, q, e), col0 + 16 * n - z.dvp), kOperand, S[n][e]);
+                for (int e = 0; e < 4; ++e) P[transition_place<DK>(state_row(wave, q, e), col0 + 16 * n - z.dvp)] = S[n][e];
         } else {
             put_to(a.out_add + g * one);
         }
@@ -932,8 +934,8 @@ __device__ __forceinline__ float sum_lanes(float (&v)[N], int lane)
 // (and with dk <= 64 half of the tokens), for which it reads its rows of S and dS once, as right operands: dO S^T, dR S^T and U dS^T.  F and E are
 // formed from the same tiles before these are overwritten with F, F^T and E + E^T, whose products with K and Q end the kernel.  A workgroup goes on to the
 // chunk before it, whose states it has asked for by then; <S', dS> takes S' from the chunk behind.
-// 4096 chunks of dk = dv = 128, bf16: 382 us for 288 KB a chunk, 3.1 TB/s.  LDS holds one workgroup of a CU, which waits for its own reading: wavefronts wait 43 % of
-// their time (matrix units busy 14 %, vector ALU 42 %).
+// 4096 chunks of dk = dv = 128, bf16: 342 us for 288 KB a chunk, 3.5 TB/s.  LDS holds one workgroup of a CU, which waits for its own reading at the chunk's start
+// and for tiles in LDS after that.
 constexpr int kGradThreads = 512;
 
 template <class X, int DK>
@@ -1425,8 +1427,8 @@ struct Passes {
         a.final_state = floats(ws, p.off_add) + z.seg0 * one;
         a.final_head = one * p.nseg;
         a.transitions = 1;
-        a.P = ws + p.off_P;
-        a.PT = ws + p.off_PT;
+        a.P = floats(ws, p.off_P);
+        a.PT = floats(ws, p.off_PT);
         const dim3 grid((p.dvp / 16 + DK / 16 + kTiles - 1) / kTiles, segs, p.BH);
         DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, THREADS, kPre>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
         return hipSuccess;
@@ -1441,7 +1443,7 @@ struct Passes {
         a.groups = 1;
         a.each = a.steps = steps;
         a.first = rev ? z.seg0 + z.segs - 1 : z.seg0;
-        a.P = ws + (rev ? p.off_PT : p.off_P);
+        a.P = floats(ws, rev ? p.off_PT : p.off_P);
         a.p_head = p.nseg;
         a.add = floats(ws, p.off_add);
         a.carry = carry;
@@ -1456,7 +1458,7 @@ struct Passes {
             c.each = each;
             c.carry = nullptr;
             c.at = nullptr;
-            c.out_P = ws + p.off_group_P;
+            c.out_P = floats(ws, p.off_group_P);
             c.out_add = floats(ws, p.off_group_add);
             c.out_head = p.join_groups;
             if (hipError_t e = launch_combine(c, rev, st); e != hipSuccess) return e;

@@ -77,7 +77,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         *pl = p;
         return RACE_OK;
     }
-    const size_t dkp = d->dk <= 64 ? 64 : 128, split = d->dtype == RACE_F32 ? 4 : 6, one = sizeof(float) * p.dk * p.dv, square = kChunk * kChunk;
+    const size_t dkp = d->dk <= 64 ? 64 : 128, one = sizeof(float) * p.dk * p.dv, square = kChunk * kChunk;
     const size_t per_chunk = square * 4 + 5 * kChunk * 4 + (backward ? square * 8 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
     const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
@@ -103,12 +103,12 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     const size_t segs = static_cast<size_t>(p.BH) * p.nseg;
     if (p.win_segs > 1) {
         p.off_add = take(segs * one);
-        p.off_P = take(segs * dkp * dkp * split);
-        p.off_PT = take(segs * dkp * dkp * split);
+        p.off_P = take(segs * dkp * dkp * 4);
+        p.off_PT = take(segs * dkp * dkp * 4);
     }
     if (p.win_segs > kJoinInGroups) {
         p.join_groups = static_cast<int>(std::lround(std::sqrt(static_cast<double>(p.win_segs))));
-        p.off_group_P = take(static_cast<size_t>(p.BH) * p.join_groups * dkp * dkp * split);
+        p.off_group_P = take(static_cast<size_t>(p.BH) * p.join_groups * dkp * dkp * 4);
         p.off_group_add = take(static_cast<size_t>(p.BH) * p.join_groups * one);
         p.off_group_start = take(static_cast<size_t>(p.BH) * p.join_groups * one);
     }
