@@ -41,7 +41,7 @@ race_status_t check_delta(const race_delta_desc_t *d)
 
 // Segments that run side by side, by the time of a forward pass, in us, from sweeps at dk = dv = 128 (bf16; the other shapes have their minimum
 // in the same places): a chunk takes 7.2 in the pass proper, with a workgroup per segment and head, and 4.4 in the pre-pass, with two; the CUs hold
-// 256 workgroups at once; the join takes 3 a segment one after the other, in groups 25 + 0.7 a segment.  At B H = 4 and 1024 chunks, training: 64 segments
+// 256 workgroups at once; the join takes 2 to 3 a segment one after the other, in groups 25 + 0.7 a segment.  At B H = 4 and 1024 chunks, training: 64 segments
 // 1521, 61: 1556, 52: 1660, 43: 1807, 32: 1895, 74 (a second round): 1931.
 int choose_segments(int chunks, int BH)
 {
