@@ -1,6 +1,9 @@
 """Thin binding of librace_attn.so: argument marshalling only.  Every step of the path runs in the library's HIP kernels;
 torch is used for device memory and streams.  Names follow include/race_attn.h.  The calls of a training or serving loop go
 through the extension module _native (csrc/native_binding.cpp), the rest through ctypes.
+
+stream: None is the current stream, else a torch stream or a raw handle.  Scratch and outputs that a call makes itself belong to the call's stream; tensors
+that it is given have to be ready there, and to stay until it has used them.
 """
 from __future__ import annotations
 
@@ -167,11 +170,39 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _workspace(desc, workspace, device):
+def _owned(stream, make, returned: bool = True):
+    """Device memory that a call on `stream` uses: allocated for that stream, so that the allocator hands it on only behind the call's work; a tensor that
+    is returned is kept from reuse until the current stream's work on it is done, too."""
+    if stream is None:
+        return make()
+    cuda = _torch().cuda
+    here = cuda.current_stream()
+    if not isinstance(stream, cuda.Stream):
+        raw = _stream(stream)
+        stream = cuda.ExternalStream(raw) if raw else cuda.default_stream()
+    with cuda.stream(stream):
+        made = make()
+    if returned and made.is_cuda:
+        made.record_stream(here)
+    return made
+
+
+def _empty(stream, shape, dtype, device):
+    return _owned(stream, lambda: _torch().empty(shape, dtype=dtype, device=device))
+
+
+def _like(stream, x):
+    return _owned(stream, lambda: _torch().empty_like(x))
+
+
+def _scratch(need, device, stream):
     torch = _torch()
-    need = race_attn_workspace_bytes(desc)
+    return _owned(stream, lambda: torch.empty(max(need, 256), dtype=torch.uint8, device=device), returned=False)
+
+
+def _workspace(desc, workspace, device, stream):
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        workspace = _scratch(race_attn_workspace_bytes(desc), device, stream)
     return workspace, workspace.numel()
 
 
@@ -203,10 +234,10 @@ def race_attn_fwd(desc: RaceAttnDesc, Q, K, V, proj_seeds: Sequence[int], O=None
         for t, n in ((Q, "Q"), (K, "K"), (V, "V")):
             _check_tensor(t, desc, n)
         if O is None:
-            O = torch.empty_like(V)
+            O = _like(stream, V)
         if den is None:
-            den = torch.empty((desc.B, desc.H, desc.N), dtype=torch.float32, device=V.device)
-        workspace, _ = _workspace(desc, workspace, V.device)
+            den = _empty(stream, (desc.B, desc.H, desc.N), torch.float32, V.device)
+        workspace, _ = _workspace(desc, workspace, V.device, stream)
     st = (_native_module or _native()).fwd(desc, Q, K, V, proj_seeds, O, den, workspace, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_attn_fwd")
@@ -223,22 +254,20 @@ def race_attn_fwd_static(desc: RaceAttnDesc, Q, K, V, proj_seeds: Sequence[int],
 
 def _backward(where, saved, desc, Q, K, V, O, den, dO, proj_seeds, dQ, dK, dV, dbeta, workspace, stream):
     if dQ is None or dK is None or dV is None or workspace is None:
-        torch = _torch()
         for t, n in ((Q, "Q"), (K, "K"), (V, "V"), (O, "O"), (dO, "dO")):
             _check_tensor(t, desc, n)
-        dQ = torch.empty_like(Q) if dQ is None else dQ
-        dK = torch.empty_like(K) if dK is None else dK
-        dV = torch.empty_like(V) if dV is None else dV
-        workspace, _ = _workspace(desc, workspace, V.device)
+        dQ = _like(stream, Q) if dQ is None else dQ
+        dK = _like(stream, K) if dK is None else dK
+        dV = _like(stream, V) if dV is None else dV
+        workspace, _ = _workspace(desc, workspace, V.device, stream)
     st = (_native_module or _native()).bwd(desc, Q, K, V, O, den, dO, proj_seeds, dQ, dK, dV, dbeta, workspace, stream, saved)
     if st != RACE_OK:
         raise RaceAttnError(st, where)
     return dQ, dK, dV
 
 
-def _new_dbeta(desc, V):
-    torch = _torch()
-    return torch.empty((desc.B, desc.H), dtype=torch.float32, device=V.device)
+def _new_dbeta(desc, V, stream):
+    return _empty(stream, (desc.B, desc.H), _torch().float32, V.device)
 
 
 def race_attn_bwd(desc: RaceAttnDesc, Q, K, V, O, den, dO, proj_seeds: Sequence[int], dQ=None, dK=None, dV=None,
@@ -249,7 +278,7 @@ def race_attn_bwd(desc: RaceAttnDesc, Q, K, V, O, den, dO, proj_seeds: Sequence[
 def race_attn_bwd_beta(desc: RaceAttnDesc, Q, K, V, O, den, dO, proj_seeds: Sequence[int], dQ=None, dK=None, dV=None,
                        dbeta=None, workspace=None, stream=None):
     """race_attn_bwd plus the cotangent of the temperature per (batch, head): returns dQ, dK, dV, dbeta (B, H)."""
-    dbeta = _new_dbeta(desc, V) if dbeta is None else dbeta
+    dbeta = _new_dbeta(desc, V, stream) if dbeta is None else dbeta
     return _backward("race_attn_bwd_beta", False, desc, Q, K, V, O, den, dO, proj_seeds, dQ, dK, dV, dbeta, workspace,
                      stream) + (dbeta,)
 
@@ -261,7 +290,7 @@ def race_attn_bwd_saved(desc: RaceAttnDesc, Q, K, V, O, den, dO, proj_seeds: Seq
     if workspace is None:
         raise ValueError("race_attn_bwd_saved needs the workspace the forward pass wrote")
     if dbeta is None and want_dbeta:
-        dbeta = _new_dbeta(desc, V)
+        dbeta = _new_dbeta(desc, V, stream)
     grads = _backward("race_attn_bwd_saved", True, desc, Q, K, V, O, den, dO, proj_seeds, dQ, dK, dV, dbeta, workspace, stream)
     return grads + (dbeta,) if dbeta is not None else grads
 
@@ -270,10 +299,9 @@ def race_attn_debug_hash(desc: RaceAttnDesc, X, proj_seeds: Sequence[int], want_
                          workspace=None, stream=None):
     torch = _torch()
     _check_tensor(X, desc, "X")
-    codes = torch.empty((desc.B, desc.H, desc.N, desc.L), dtype=torch.uint8, device=X.device)
-    phi = torch.empty((desc.B, desc.H, desc.N, desc.L, 1 << desc.P), dtype=torch.float32,
-                      device=X.device) if want_phi else None
-    workspace, nbytes = _workspace(desc, workspace, X.device)
+    codes = _empty(stream, (desc.B, desc.H, desc.N, desc.L), torch.uint8, X.device)
+    phi = _empty(stream, (desc.B, desc.H, desc.N, desc.L, 1 << desc.P), torch.float32, X.device) if want_phi else None
+    workspace, nbytes = _workspace(desc, workspace, X.device, stream)
     st = lib().race_attn_debug_hash(ctypes.byref(desc), X.data_ptr(), _seeds(proj_seeds), codes.data_ptr(),
                                     phi.data_ptr() if want_phi else None, workspace.data_ptr(), nbytes,
                                     _stream(stream))
@@ -287,9 +315,9 @@ def race_attn_debug_buckets(desc: RaceAttnDesc, K, V, proj_seeds: Sequence[int],
     _check_tensor(K, desc, "K")
     _check_tensor(V, desc, "V")
     R = 1 << desc.P
-    A = torch.empty((desc.B, desc.H, desc.L, R), dtype=torch.float32, device=K.device)
-    Bsum = torch.empty((desc.B, desc.H, desc.L, R, desc.d), dtype=torch.float32, device=K.device)
-    workspace, nbytes = _workspace(desc, workspace, K.device)
+    A = _empty(stream, (desc.B, desc.H, desc.L, R), torch.float32, K.device)
+    Bsum = _empty(stream, (desc.B, desc.H, desc.L, R, desc.d), torch.float32, K.device)
+    workspace, nbytes = _workspace(desc, workspace, K.device, stream)
     st = lib().race_attn_debug_buckets(ctypes.byref(desc), K.data_ptr(), V.data_ptr(), _seeds(proj_seeds),
                                        A.data_ptr(), Bsum.data_ptr(), workspace.data_ptr(), nbytes, _stream(stream))
     if st != RACE_OK:
@@ -306,11 +334,11 @@ def race_attn_state_init(desc: RaceAttnDesc, K, V, proj_seeds: Sequence[int], st
     torch = _torch()
     shape = (desc.B, desc.H, desc.L, 1 << desc.P, desc.d + 1)
     device = K.device if K is not None else (state.device if state is not None else "cuda")
-    state = torch.empty(shape, dtype=torch.float32, device=device) if state is None else state
+    state = _empty(stream, shape, torch.float32, device) if state is None else state
     if desc.N > 0 and workspace is None:
         _check_tensor(K, desc, "K")
         _check_tensor(V, desc, "V")
-        workspace, _ = _workspace(desc, workspace, K.device)
+        workspace, _ = _workspace(desc, workspace, K.device, stream)
     st = (_native_module or _native()).state_init(desc, K, V, proj_seeds, state, workspace if desc.N > 0 else None, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_attn_state_init")
@@ -330,12 +358,12 @@ def race_attn_step(desc: RaceAttnDesc, q, k, v, proj_seeds: Sequence[int], state
         row = (desc.B, desc.H, desc.d)
         for t, n in ((q, "q"), (k, "k"), (v, "v")):
             _check_tensor(t, desc, n, row)
-        o = torch.empty_like(v) if o is None else o
-        den = torch.empty((desc.B, desc.H), dtype=torch.float32, device=v.device) if den is None else den
+        o = _like(stream, v) if o is None else o
+        den = _empty(stream, (desc.B, desc.H), torch.float32, v.device) if den is None else den
         if workspace is None:
             if proj_seeds is None:
                 raise ValueError("race_attn_step without seeds needs the workspace of an earlier step")
-            workspace = torch.empty(race_attn_step_workspace_bytes(desc), dtype=torch.uint8, device=v.device)
+            workspace = _scratch(race_attn_step_workspace_bytes(desc), v.device, stream)
     st = (_native_module or _native()).step(desc, q, k, v, proj_seeds, state, o, den, workspace, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_attn_step")
@@ -398,19 +426,15 @@ def race_delta_segment_tokens(desc: RaceDeltaDesc) -> int:
     return int(lib().race_delta_segment_tokens(ctypes.byref(desc)))
 
 
-def _scratch(need, device):
-    return _torch().empty(max(need, 256), dtype=_torch().uint8, device=device)
-
-
 def race_delta_fwd(desc: RaceDeltaDesc, Q, K, V, g, beta, state_in=None, O=None, state_out=None, want_state: bool = False, workspace=None,
                    stream=None):
     """Returns O (B, H, N, dv) and the state behind the sequence, (B, H, dk, dv) float32 (None unless state_out or want_state is given)."""
     if O is None:
-        O = _torch().empty_like(V)
+        O = _like(stream, V)
     if state_out is None and want_state:
-        state_out = _torch().empty((desc.B, desc.H, desc.dk, desc.dv), dtype=_torch().float32, device=V.device)
+        state_out = _empty(stream, (desc.B, desc.H, desc.dk, desc.dv), _torch().float32, V.device)
     if workspace is None:
-        workspace = _scratch(race_delta_workspace_bytes(desc), V.device)
+        workspace = _scratch(race_delta_workspace_bytes(desc), V.device, stream)
     st = (_native_module or _native()).delta_fwd(desc, Q, K, V, g, beta, state_in, O, state_out, workspace, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_delta_fwd")
@@ -420,12 +444,11 @@ def race_delta_fwd(desc: RaceDeltaDesc, Q, K, V, g, beta, state_in=None, O=None,
 def race_delta_bwd(desc: RaceDeltaDesc, Q, K, V, g, beta, dO, state_in=None, dstate_out=None, dQ=None, dK=None, dV=None, dg=None, dbeta=None,
                    dstate_in=None, want_dstate: bool = False, workspace=None, stream=None):
     """Returns dQ, dK, dV, dg, dbeta and the cotangent of state_in (None unless dstate_in or want_dstate is given)."""
-    torch = _torch()
-    dQ, dK, dV, dg, dbeta = (torch.empty_like(x) if y is None else y for x, y in ((Q, dQ), (K, dK), (V, dV), (g, dg), (beta, dbeta)))
+    dQ, dK, dV, dg, dbeta = (_like(stream, x) if y is None else y for x, y in ((Q, dQ), (K, dK), (V, dV), (g, dg), (beta, dbeta)))
     if dstate_in is None and want_dstate:
-        dstate_in = torch.empty((desc.B, desc.H, desc.dk, desc.dv), dtype=torch.float32, device=V.device)
+        dstate_in = _empty(stream, (desc.B, desc.H, desc.dk, desc.dv), _torch().float32, V.device)
     if workspace is None:
-        workspace = _scratch(race_delta_bwd_workspace_bytes(desc), V.device)
+        workspace = _scratch(race_delta_bwd_workspace_bytes(desc), V.device, stream)
     st = (_native_module or _native()).delta_bwd(desc, Q, K, V, g, beta, state_in, dO, dstate_out, dQ, dK, dV, dg, dbeta, dstate_in, workspace, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_delta_bwd")
@@ -435,7 +458,7 @@ def race_delta_bwd(desc: RaceDeltaDesc, Q, K, V, g, beta, dO, state_in=None, dst
 def race_delta_step(desc: RaceDeltaDesc, q, k, v, g, beta, state, o=None, stream=None):
     """One token: q, k (B, Hk, dk), v (B, H, dv), g, beta (B, H); the state is updated in place; returns o (B, H, dv)."""
     if o is None:
-        o = _torch().empty_like(v)
+        o = _like(stream, v)
     st = (_native_module or _native()).delta_step(desc, q, k, v, g, beta, state, o, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_delta_step")
@@ -462,9 +485,9 @@ def race_qk_rotary_workspace_bytes(desc: RaceRotaryDesc) -> int:
 def race_qk_rotary_fwd(desc: RaceRotaryDesc, q, k, wq, wk, inv_freq: Sequence[float], positions=None, Q=None, K=None, stream=None):
     """q (B, N, Hq, d) and k (B, N, Hk, d), views with any strides but 1 in the last dimension; returns Q (B, Hq, N, d) and K (B, Hk, N, d)."""
     if Q is None:
-        Q = _torch().empty((desc.B, desc.Hq, desc.N, desc.d), dtype=q.dtype, device=q.device)
+        Q = _empty(stream, (desc.B, desc.Hq, desc.N, desc.d), q.dtype, q.device)
     if K is None and desc.Hk > 0:
-        K = _torch().empty((desc.B, desc.Hk, desc.N, desc.d), dtype=k.dtype, device=k.device)
+        K = _empty(stream, (desc.B, desc.Hk, desc.N, desc.d), k.dtype, k.device)
     st = (_native_module or _native()).rotary_fwd(desc, q, k, wq, wk, inv_freq, positions, Q, K, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_qk_rotary_fwd")
@@ -474,14 +497,13 @@ def race_qk_rotary_fwd(desc: RaceRotaryDesc, q, k, wq, wk, inv_freq: Sequence[fl
 def race_qk_rotary_bwd(desc: RaceRotaryDesc, q, k, wq, wk, inv_freq: Sequence[float], positions, dQ, dK, dq=None, dk=None, dwq=None, dwk=None,
                        workspace=None, stream=None):
     """Returns dq, dk in the layout (B, N, heads, d) (views with strides of their own if given) and dwq, dwk (None without weights)."""
-    torch = _torch()
     keys = desc.Hk > 0
-    dq = torch.empty((desc.B, desc.N, desc.Hq, desc.d), dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty((desc.B, desc.N, desc.Hk, desc.d), dtype=k.dtype, device=k.device) if dk is None and keys else dk
-    dwq = torch.empty_like(wq) if dwq is None and wq is not None else dwq
-    dwk = torch.empty_like(wk) if dwk is None and wk is not None and keys else dwk
+    dq = _empty(stream, (desc.B, desc.N, desc.Hq, desc.d), q.dtype, q.device) if dq is None else dq
+    dk = _empty(stream, (desc.B, desc.N, desc.Hk, desc.d), k.dtype, k.device) if dk is None and keys else dk
+    dwq = _like(stream, wq) if dwq is None and wq is not None else dwq
+    dwk = _like(stream, wk) if dwk is None and wk is not None and keys else dwk
     if workspace is None and (dwq is not None or dwk is not None):
-        workspace = _scratch(race_qk_rotary_workspace_bytes(desc), q.device)
+        workspace = _scratch(race_qk_rotary_workspace_bytes(desc), q.device, stream)
     st = (_native_module or _native()).rotary_bwd(desc, q, k, wq, wk, inv_freq, positions, dQ, dK, dq, dk, dwq, dwk, workspace, stream)
     if st != RACE_OK:
         raise RaceAttnError(st, "race_qk_rotary_bwd")
