@@ -225,8 +225,10 @@ race_status_t race_attn_step(const race_attn_desc_t *desc, const void *q, const 
  *     g, beta, dg, dbeta are DEVICE float (B, H, N); states are DEVICE float (B, H, dk, dv).  Value head h reads the queries and keys of
  *     head h / (H / Hk); their gradients are summed over the value heads that share them.
  *   - g is the logarithm of the decay, usually <= 0; -infinity (every value below -1e5) empties the state before the token is written.  beta is
- *     used as given.  Rows of Q and K are used as given: a bounded state wants |k| <= 1 with beta in [0, 2] (race_qk_rotary_fwd makes such rows).
- *   - A padding token is one with g = 0 and beta = 0: the state passes it unchanged; its rows must be finite.
+ *     used as given (0 where |beta| < 2^-100).  Rows of Q and K are used as given: a bounded state wants |k| <= 1 with beta in [0, 2] (race_qk_rotary_fwd makes such rows).
+ *   - A padding token is one with g = 0 and beta = 0: the state passes it unchanged, whatever its rows of K and V hold, as long as it is finite, and so do the other tokens'
+ *     outputs and, where its dO is 0, gradients.  Its own output reads the state with its query, whose products with keys and states have to stay finite.
+ *     Its rows of dK and dV are 0; its dbeta is what the formula makes of its rows.
  *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64; a sum over part of 64 tokens has to stay
  *     below 88, where exp leaves fp32).  The bf16 type multiplies fp32 values as sums of three bf16, all 24 bits (of two where only a bf16 output depends
  *     on the product); O, dQ, dK and dV are rounded to bf16 at the end.

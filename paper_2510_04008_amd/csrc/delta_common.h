@@ -20,8 +20,12 @@
 //     dG_i = q_i.dQ_i - v_i.dV_i,   dg_t = sum_{i >= t, in the chunk} dG_i + <S', dS>
 // The last line: with S_t = e^{G_t} Z_t the recurrence of Z holds no decay, only v_t e^{-G_t} and o_t e^{G_t} do, so the cotangent of
 // G_t is o_t.dO_t - v_t.dV_t, and o is linear in q; a chunk's sum starts from the inner product at its end, which
-// keeps rounding errors from adding up along the sequence.  db divides by b: tokens with b = 0 are computed with b = 1e-18
-// throughout, far below any rounding, and u_i / b_i is then their error row to full precision.
+// keeps rounding errors from adding up along the sequence.
+// Tokens of strength zero (padding; |b| below 2^-100 counts as that) write nothing, whatever finite values their rows hold: their rows of A and of
+// b (V - e^G K S) are zeros, not products with zero.  db divides by b; for them it is v_i.dR_i + k_i.X_i with
+//     X_i = -sum_j D_ij (dR_i.u_j) k_j - e^{G_i} S dR_i,
+// which is their row of (E K - b e^G dR S^T) for b = 1, and not part of dK.  dR_i hangs on their keys alone; what these make of A's and M's columns and
+// of dR is kept within 2^60, so that it stays finite where it meets a zero.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -41,7 +45,7 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any4;
 
 constexpr int C = 64;               // tokens per chunk
 constexpr int kDec = 5 * C;         // decays and strengths of a chunk
-constexpr float kBetaFloor = 1e-18f;
+constexpr float kBetaFloor = 0x1p-100f, kIdleMax = 0x1p60f;
 constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 0 either way, and -infinity would make differences NaN
 
 // Element types.  The passes over the states multiply 16 x 16 tiles, 32 deep: lane l holds row (of a left operand) or column (of a right one)
@@ -347,7 +351,9 @@ __device__ __forceinline__ int spread(int k) { return (k & ~31) | ((k & 12) << 1
 __device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
 __device__ __forceinline__ float gate(float g) { return g < kGateFloor ? kGateFloor : g; }       // NaN stays
-__device__ __forceinline__ float strength(float b) { return fabsf(b) < kBetaFloor ? kBetaFloor : b; }
+__device__ __forceinline__ float strength(float b) { return fabsf(b) < kBetaFloor ? 0.f : b; }       // NaN stays
+// what hangs on the rows of a token of strength zero
+__device__ __forceinline__ float idle(float x) { return fminf(fmaxf(x, -kIdleMax), kIdleMax); }
 
 // exp(G_i - G_j) of sums that are held as two floats each: their difference is exact to fp32 however large they are
 __device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float lo_j)

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     if (wave == 3) {
         const int64_t t = static_cast<int64_t>(bh) * z.N + t0 + lane;
         const double g = prefix64(lane < n ? static_cast<double>(gate(a.g[t])) : 0.0, lane);
-        const float b = lane < n ? strength(a.beta[t]) : kBetaFloor, hi = static_cast<float>(g);
+        const float b = lane < n ? strength(a.beta[t]) : 0.f, hi = static_cast<float>(g);
         hi_of[lane] = hi;
         lo_of[lane] = static_cast<float>(g - hi);
         B[lane] = b;
@@ -137,6 +137,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
         float *MT = a.MT + at * C * C + (32 * tj + col) * C + 32 * ti;
         const int j = 32 * tj + col;
         const float hj = hi_of[j], lj = lo_of[j];
+        const bool idle_j = B[j] == 0.f;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
             const int i0 = 32 * ti + acc_row(4 * e4, h);
@@ -145,8 +146,9 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float D = decay(hi[e], lo[e], hj, lj), x = z.scale * D * qk[4 * e4 + e], y = b[e] * D * kk[4 * e4 + e];
-                m[e] = j <= i0 + e ? x : 0.f;
-                A[i0 + e][j] = j < i0 + e ? y : 0.f;
+                m[e] = j <= i0 + e ? (idle_j ? idle(x) : x) : 0.f;
+                // (the column of a token of strength zero meets its zeros; only its own cotangent reads it)
+                A[i0 + e][j] = j < i0 + e && b[e] != 0.f ? (idle_j ? (BWD ? idle(y) : 0.f) : y) : 0.f;
             }
             if (BWD) *reinterpret_cast<f32x4 *>(MT + spread(acc_row(4 * e4, h))) = m;
         }
@@ -314,7 +316,7 @@ struct ColumnsStage {
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) x[ti] = load8(p + static_cast<int64_t>(min(16 * ti + (lane & 15), n - 1)) * width + (k < width ? k : 0), true);
     }
-    // Rows behind the last token repeat it: their strengths are 1e-18 and their keys and queries zero.  Columns that there are not are zeros of `unit`.
+    // Rows behind the last token repeat it: their strengths, keys and queries are zero.  Columns that there are not are zeros of `unit`.
     static __device__ __forceinline__ typename X::Exact unit(int width, int k0, int lane)
     {
         return or_zero(unit8<X, false>(0, lane), k0 + 8 * ((lane >> 4) & 1) < width);
@@ -501,10 +503,11 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
                 for (int kb = 0; kb < DK / 32; ++kb) m = mma(tile8<X, L::kRow>(Ks, 16 * tj, 32 * kb, lane), tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), m);
                 const float hi = dec[3 * C + i], lo = dec[4 * C + i];
                 const f32x4 hj = *reinterpret_cast<const f32x4 *>(dec + 3 * C + j0), lj = *reinterpret_cast<const f32x4 *>(dec + 4 * C + j0);
+                const f32x4 bj = *reinterpret_cast<const f32x4 *>(beta + j0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float x = z.scale * decay(hi, lo, hj[e], lj[e]) * m[e];
-                    m[e] = j0 + e <= i ? x : 0.f;
+                    m[e] = j0 + e <= i && bj[e] != 0.f ? x : 0.f;
                 }
                 put4_pair(Ms + i * L::kTok + spread(j0), L::kSquare, m);
             }
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
             const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + 16 * ti + 4 * q), b = *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                R[ti][e] = b[e] * (v[e] - g[e] * R[ti][e]);
+                R[ti][e] = b[e] != 0.f ? b[e] * (v[e] - g[e] * R[ti][e]) : 0.f;
                 if (MODE == kOut) O[ti][e] *= z.scale * g[e];
             }
         }
@@ -840,6 +843,13 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 #pragma unroll
             for (int ti = 0; ti < 2 * kb + 2; ++ti) U[ti] = mma(tile8s<Split, L::kTok>(Ms, 16 * ti, 32 * kb, lane), o, U[ti]);
         }
+        auto strengths = [&](int ti) { return *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q); };
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti) {
+            const f32x4 b = strengths(ti);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) U[ti][e] = b[e] != 0.f ? U[ti][e] : idle(U[ti][e]);
+        }
         fence();
         // dR = T^T dU = dU + (T^T - I) dU
         f32x4 R[4];
@@ -852,7 +862,6 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 #pragma unroll
             for (int ti = 0; ti < 2 * kb + 2; ++ti) R[ti] = mma(tile8s<Split, L::kTok>(Ts, 16 * ti, 32 * kb, lane), u, R[ti]);
         }
-        auto strengths = [&](int ti) { return *reinterpret_cast<const f32x4 *>(beta + 16 * ti + 4 * q); };
         if (FULL) {
             float *keep = a.dR + at * C * z.dvp;
             E *dV = static_cast<E *>(a.dV) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
@@ -947,7 +956,7 @@ struct GradLds {
     static constexpr int kFloats = kDec + 8 * C + C + 8;                // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
     static constexpr int kTiles = C * kWide * (X::kPlanes + X::kPairPlanes + (kHasO ? 1 : 0));
     static constexpr size_t kBytes = kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
-    static_assert((X::kPlanes + 2 * X::kPairPlanes) * L::kSquare <= kTiles, "F, F^T and E + E^T lie where U, dR and dO were");
+    static_assert((X::kPlanes + 2 * X::kPairPlanes) * L::kSquare * sizeof(E) + 8 * C * sizeof(float) <= kTiles * sizeof(E), "F, F^T, E + E^T and k.X lie where U, dR and dO were");
 };
 
 template <class X, int DK>
@@ -964,6 +973,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     float *eG = reinterpret_cast<float *>(lds_raw), *eEnd = eG + C, *bs = eEnd + C, *hi_of = bs + C, *lo_of = hi_of + C, *qd = lo_of + C, *vd = qd + 8 * C, *part = vd + C;
     E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPairPlanes * C * kWide;
     E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
+    float *kd = reinterpret_cast<float *>(Es + X::kPairPlanes * L::kSquare);        // k.X of eight wavefronts
     const Sizes &z = a.z;
     const int wave = wave_index();
     int tid = threadIdx.x;
@@ -1034,6 +1044,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
         if (has_k || has_q) rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
         __syncthreads();                        // the strengths
+        const bool idle_tokens = __any(lane < n && bs[lane] == 0.f);
         // the tiles, and on the way u.dR and v.dR of every token; over the states <S', dS>
         float dot = 0.f;
 #pragma unroll
@@ -1066,8 +1077,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 vr += __shfl_xor(vr, m);
             }
             if ((tid & 15) == 0) {
-                vd[i] = bs[i] * vr;
-                if (i < n) a.dbeta[row0 + i] = ud / bs[i];
+                vd[i] = vr;
+                if (i < n && bs[i] != 0.f) a.dbeta[row0 + i] = ud / bs[i];
             }
         }
         __syncthreads();
@@ -1101,7 +1112,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 }
             }
         }
-        // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T
+        // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T (b = 0: X's part)
         f32x4 dq[TI], dk[TI], y[TI];
 #pragma unroll
         for (int t = 0; t < TI; ++t) dq[t] = dk[t] = y[t] = zero4();
@@ -1146,11 +1157,14 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         for (int t = 0; t < TI; ++t) {
             const int i = 16 * (ti0 + t) + 4 * q;
             const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + i), b = *reinterpret_cast<const f32x4 *>(bs + i);
+            f32x4 b1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b1[e] = b[e] != 0.f ? b[e] : 1.f;
             dq[t] *= z.scale * g;
-            dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b * g * y[t];
+            dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b1 * g * y[t];
         }
         __syncthreads();
-        // F, its transpose, and E + E^T
+        // F, its transpose, and E + E^T (b = 0: the row of X, and nothing in E^T)
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
             const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
@@ -1171,7 +1185,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) put1_pair(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
             } else {
-                const f32x4 x = -bs[i] * D * jobs[k];
+                const bool idle_i = bs[i] == 0.f;
+                const f32x4 x = (idle_i ? -1.f : -bs[i]) * D * jobs[k];
                 f32x4 x0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x0[e] = j0 + e < i ? x[e] : 0.f;
@@ -1179,7 +1194,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 // after the rows: in a diagonal tile these places hold its zeros
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, x[e]);
+                    if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, idle_i ? 0.f : x[e]);
             }
         }
         fence();
@@ -1219,18 +1234,29 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 if (kNext) fence();
             }
         }
-        {
+        // a row's elements times those of a gradient, summed over the wavefront's columns
+        auto row_dots = [&](const E *rows, const f32x4 (&grad)[TI], float *to) {
             float v[4 * TI];
 #pragma unroll
             for (int t = 0; t < TI; ++t) {
                 float x[4];
-                get4(Qt + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
+                get4(rows + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * dq[t][e];
+                for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * grad[t][e];
             }
             const float s = sum_lanes(v, lane);
             const int w = col % (4 * TI);
-            if (col < 4 * TI) qd[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
+            if (col < 4 * TI) to[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
+        };
+        row_dots(Qt, dq, qd);
+        if (idle_tokens) {
+            row_dots(Kt, dk, kd);
+#pragma unroll
+            for (int t = 0; t < TI; ++t) {
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(bs + 16 * (ti0 + t) + 4 * q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dk[t][e] = b[e] != 0.f ? dk[t][e] : 0.f;
+            }
         }
         const int d0 = dcol - col;
         if (a.shared) {
@@ -1254,11 +1280,19 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         }
         __syncthreads();
         if (wave == 0) {
-            float mine = -vd[lane], tail = 0.f;
+            const bool idle_token = bs[lane] == 0.f;
+            float mine = idle_token ? 0.f : -bs[lane] * vd[lane], tail = 0.f;
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
                 mine += qd[w * C + lane];
                 tail += part[w];
+            }
+            if (idle_token && lane < n) {
+                float b = vd[lane];
+#pragma unroll
+                for (int w = 0; w < 8; ++w)
+                    if (DK == 128 || w / (DK / 16) == lane / 32) b += kd[w * C + lane];       // (with dk <= 64 a wavefront has half of the tokens)
+                a.dbeta[row0 + lane] = b;
             }
             float s = mine;         // sum over this token and those behind it
 #pragma unroll
@@ -1318,7 +1352,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(Sizes z, const E *q, co
         ks[tid] = tid < z.dk ? value(k[row + tid]) : 0.f;
         qs[tid] = tid < z.dk ? value(q[row + tid]) : 0.f;
     }
-    const float a = expf(gate(g[bh])), b = beta[bh];
+    const float a = expf(gate(g[bh])), b = strength(beta[bh]);
     __syncthreads();
     // sum over rows: the eight row groups of a wavefront, then the four wavefronts
     auto over_rows = [&](const float *w) {
@@ -1338,7 +1372,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(Sizes z, const E *q, co
     for (int r = 0; r < 4; ++r) s[r] *= a;
     f32x4 u = over_rows(ks);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = there ? b * (value(v[static_cast<size_t>(bh) * z.dv + c0 + e]) - u[e]) : 0.f;
+    for (int e = 0; e < 4; ++e) u[e] = there && b != 0.f ? b * (value(v[static_cast<size_t>(bh) * z.dv + c0 + e]) - u[e]) : 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int i = rg + 32 * r;
