@@ -55,24 +55,21 @@ constexpr float kGateFloor = -1e5f; // log decays below act as this one: exp is 
 // K K^T and Q K^T of prep are 32 x 32 tiles, 16 deep, half as many operands to a product: lane l holds row l % 32 and the elements 8 h + 0..7, h = l / 32.
 //
 // bf16: the elements of Q, K, V and dO are exact as they are.  Values that are fp32 by their nature enter as
-// sums of bf16: three (Split: all 24 bits) where fp32 outputs (state, dg, db) hang on them, two (Pair: off by at most 2^-16) where
-// outputs of the element type alone do.  One bf16 (2^-8) would leave the fp32 outputs three digits; with two of them throughout dg was 1.5e-5 off at dk = 16,
-// with three it and the states are within 5e-7 of a computation in 64 bits.  T as a Split and not a Pair costs the passes 7 to 15 % of their time.
+// sums of three bf16 (Split: all 24 bits) in every product.  Two (2^-16) would do for outputs that are rounded to bf16 at the end, were there no cancellation in them; but
+// a value that overwrites a thousand times larger one is read back as the difference of the two.
 // fp32: eight fp32 matrix instructions a product, one for each of a lane's k.
 struct Bf {
     typedef uint16_t E;
     typedef bf16x8 Exact;
-    struct Pair { bf16x8 hi, lo; };
     struct Split { bf16x8 hi, mid, lo; };
-    static constexpr int kPlanes = 3, kPairPlanes = 2;      // of E for a value kept as a Split, as a Pair
+    static constexpr int kPlanes = 3;       // of E for a value kept as a Split
     static constexpr int kPad = 8;          // elements behind a row of a tile in LDS: 16 bytes, so that 8 rows lie in 8 places
 };
 struct Fp {
     typedef float E;
     struct Exact { float v[8]; };
-    typedef Exact Pair;
     typedef Exact Split;
-    static constexpr int kPlanes = 1, kPairPlanes = 1;
+    static constexpr int kPlanes = 1;
     static constexpr int kPad = 4;
 };
 
@@ -93,17 +90,12 @@ __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __bu
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 // the smallest terms first; terms below 2^-24 of the product are left out
 template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Exact &b, A c) { return mfma(a, b, c); }
-template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Pair &b, A c) { return mfma(a, b.hi, mfma(a, b.lo, c)); }
-template <class A> __device__ __forceinline__ A mma(const Bf::Pair &a, const Bf::Exact &b, A c) { return mfma(a.hi, b, mfma(a.lo, b, c)); }
-template <class A> __device__ __forceinline__ A mma(const Bf::Pair &a, const Bf::Pair &b, A c) { return mfma(a.hi, b.hi, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))); }
 template <class A> __device__ __forceinline__ A mma(const Bf::Exact &a, const Bf::Split &b, A c) { return mfma(a, b.hi, mfma(a, b.mid, mfma(a, b.lo, c))); }
 template <class A> __device__ __forceinline__ A mma(const Bf::Split &a, const Bf::Exact &b, A c) { return mfma(a.hi, b, mfma(a.mid, b, mfma(a.lo, b, c))); }
 template <class A> __device__ __forceinline__ A mma(const Bf::Split &a, const Bf::Split &b, A c)
 {
     return mfma(a.hi, b.hi, mfma(a.hi, b.mid, mfma(a.mid, b.hi, mfma(a.mid, b.mid, mfma(a.hi, b.lo, mfma(a.lo, b.hi, c))))));
 }
-__device__ __forceinline__ Bf::Pair lead(const Bf::Split &a) { return Bf::Pair{a.hi, a.mid}; }
-__device__ __forceinline__ const Fp::Exact &lead(const Fp::Exact &a) { return a; }
 __device__ __forceinline__ f32x4 mma(const Fp::Exact &a, const Fp::Exact &b, f32x4 c)
 {
 #pragma unroll
@@ -140,16 +132,6 @@ __device__ __forceinline__ void split8(const float *x, Bf::Split &s)
     }
     s = Bf::Split{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, mid), __builtin_bit_cast(bf16x8, lo)};
 }
-__device__ __forceinline__ void split8(const float *x, Bf::Pair &s)
-{
-    u32x4 hi, lo;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        hi[j] = round2(x[2 * j], x[2 * j + 1]);
-        lo[j] = round2(x[2 * j] - low2(hi[j]), x[2 * j + 1] - high2(hi[j]));
-    }
-    s = Bf::Pair{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
-}
 __device__ __forceinline__ void split8(const float *x, Fp::Exact &s)
 {
 #pragma unroll
@@ -174,12 +156,10 @@ __device__ __forceinline__ void put8(float *p, const Fp::Exact &x)
     reinterpret_cast<f32x4 *>(p)[0] = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
     reinterpret_cast<f32x4 *>(p)[1] = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
 }
-// a Split or a Pair lies in planes that are `plane` elements apart
+// a Split lies in planes that are `plane` elements apart
 __device__ __forceinline__ void get8(const uint16_t *p, int plane, Bf::Split &x) { x = Bf::Split{get8(p), get8(p + plane), get8(p + 2 * plane)}; }
-__device__ __forceinline__ void get8(const uint16_t *p, int plane, Bf::Pair &x) { x = Bf::Pair{get8(p), get8(p + plane)}; }
 __device__ __forceinline__ void get8(const float *p, int, Fp::Exact &x) { x = get8(p); }
 __device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Split &x) { put8(p, x.hi); put8(p + plane, x.mid); put8(p + 2 * plane, x.lo); }
-__device__ __forceinline__ void put8(uint16_t *p, int plane, const Bf::Pair &x) { put8(p, x.hi); put8(p + plane, x.lo); }
 __device__ __forceinline__ void put8(float *p, int, const Fp::Exact &x) { put8(p, x); }
 
 // four fp32 values into planes, and four elements
@@ -199,21 +179,7 @@ __device__ __forceinline__ void put4(uint16_t *p, int plane, const f32x4 &x)
     *reinterpret_cast<u32x2 *>(p + plane) = mid;
     *reinterpret_cast<u32x2 *>(p + 2 * plane) = lo;
 }
-__device__ __forceinline__ void put4_pair(uint16_t *p, int plane, const f32x4 &x)
-{
-    u32x2 hi, lo;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        hi[j] = round2(x[2 * j], x[2 * j + 1]);
-        lo[j] = round2(x[2 * j] - low2(hi[j]), x[2 * j + 1] - high2(hi[j]));
-    }
-    *reinterpret_cast<u32x2 *>(p) = hi;
-    *reinterpret_cast<u32x2 *>(p + plane) = lo;
-}
 __device__ __forceinline__ void put4(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
-__device__ __forceinline__ void put4_pair(float *p, int, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
-__device__ __forceinline__ void put4_zero(uint16_t *p) { *reinterpret_cast<u32x2 *>(p) = u32x2{0, 0}; }
-__device__ __forceinline__ void put4_zero(float *p) { *reinterpret_cast<f32x4 *>(p) = zero4(); }
 __device__ __forceinline__ void get4(const uint16_t *p, float *x)
 {
     const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
@@ -240,13 +206,6 @@ __device__ __forceinline__ void put1(uint16_t *p, int plane, float x)
     p[2 * plane] = static_cast<uint16_t>(round2(x - low2(hi) - low2(mid), 0.f));
 }
 __device__ __forceinline__ void put1(float *p, int, float x) { *p = x; }
-__device__ __forceinline__ void put1_pair(uint16_t *p, int plane, float x)
-{
-    const __bf16 hi = static_cast<__bf16>(x);
-    p[0] = __builtin_bit_cast(uint16_t, hi);
-    p[plane] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x - static_cast<float>(hi)));
-}
-__device__ __forceinline__ void put1_pair(float *p, int, float x) { *p = x; }
 __device__ __forceinline__ void values8(const Bf::Exact &x, float *f)
 {
 #pragma unroll

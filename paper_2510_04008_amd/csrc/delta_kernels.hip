@@ -421,12 +421,11 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 {
     typedef typename X::E E;
     typedef typename X::Split Split;
-    typedef typename X::Pair Pair;
     typedef Lds<X, DK> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     E *Ks = reinterpret_cast<E *>(lds_raw), *Kt = Ks + L::kByTokens, *Ts = Kt + L::kByRows, *Qs = Ts + X::kPlanes * L::kSquare;
     E *Ms = Qs + L::kByTokens;
-    float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPairPlanes * L::kSquare : Qs);
+    float *dec = reinterpret_cast<float *>(MODE == kOut ? Ms + X::kPlanes * L::kSquare : Qs);
     const Sizes &z = a.z;
     const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63, q = lane >> 4, col = lane & 15;
     const int bh = blockIdx.z, seg = blockIdx.y;
@@ -476,9 +475,9 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         take(c0);
         if (active) take_columns(c0);
     }
-    if (MODE == kOut && tid < 256) {        // what M's tiles leave out of the steps of 32 tokens on the diagonal
-        const int t = 2 * (tid >> 7), row = 16 * t + (tid >> 2 & 15), plane = tid >> 6 & 1;
-        if (plane < X::kPairPlanes) put4_zero(Ms + plane * L::kSquare + row * L::kTok + spread(16 * t + 16 + 4 * (tid & 3)));
+    if (MODE == kOut && tid < 128) {        // what M's tiles leave out of the steps of 32 tokens on the diagonal
+        const int t = 2 * (tid >> 6), row = 16 * t + (tid >> 2 & 15);
+        put4(Ms + row * L::kTok + spread(16 * t + 16 + 4 * (tid & 3)), L::kSquare, zero4());
     }
     for (int c = c0; c < c1; ++c) {
         const int64_t t0 = static_cast<int64_t>(z.chunk0 + c) * C;
@@ -509,7 +508,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
                     const float x = z.scale * decay(hi, lo, hj[e], lj[e]) * m[e];
                     m[e] = j0 + e <= i && bj[e] != 0.f ? x : 0.f;
                 }
-                put4_pair(Ms + i * L::kTok + spread(j0), L::kSquare, m);
+                put4(Ms + i * L::kTok + spread(j0), L::kSquare, m);
             }
             fence();
         }
@@ -527,7 +526,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
                 R[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, R[ti]);
-                if (MODE == kOut) O[ti] = mma(tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), lead(s), O[ti]);
+                if (MODE == kOut) O[ti] = mma(tile8<X, L::kRow>(Qs, 16 * ti, 32 * kb, lane), s, O[ti]);
             }
         }
         fence();
@@ -562,9 +561,9 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
             E *out = static_cast<E *>(a.O) + (static_cast<int64_t>(bh) * z.N + t0) * z.dv;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const Pair u = operand<Pair>(U[2 * kb], U[2 * kb + 1]);
+                const Split u = operand<Split>(U[2 * kb], U[2 * kb + 1]);
 #pragma unroll
-                for (int ti = 2 * kb; ti < 4; ++ti) O[ti] = mma(tile8s<Pair, L::kTok>(Ms, 16 * ti, 32 * kb, lane), u, O[ti]);
+                for (int ti = 2 * kb; ti < 4; ++ti) O[ti] = mma(tile8s<Split, L::kTok>(Ms, 16 * ti, 32 * kb, lane), u, O[ti]);
                 store_rows<X>(out, 32 * kb, n, z.dv, 16 * tile, O[2 * kb], O[2 * kb + 1], lane);
             }
         }
@@ -954,9 +953,9 @@ struct GradLds {
     static constexpr int kWide = 128 + X::kPad;                         // a token's row over columns of the state, in spread order
     static constexpr bool kHasO = sizeof(E) == 2;                       // dO has no room beside fp32 tiles: its operands come from memory
     static constexpr int kFloats = kDec + 8 * C + C + 8;                // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
-    static constexpr int kTiles = C * kWide * (X::kPlanes + X::kPairPlanes + (kHasO ? 1 : 0));
+    static constexpr int kTiles = C * kWide * (2 * X::kPlanes + (kHasO ? 1 : 0));
     static constexpr size_t kBytes = kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
-    static_assert((X::kPlanes + 2 * X::kPairPlanes) * L::kSquare * sizeof(E) + 8 * C * sizeof(float) <= kTiles * sizeof(E), "F, F^T, E + E^T and k.X lie where U, dR and dO were");
+    static_assert(3 * X::kPlanes * L::kSquare * sizeof(E) + 8 * C * sizeof(float) <= kTiles * sizeof(E), "F, F^T, E + E^T and k.X lie where U, dR and dO were");
 };
 
 template <class X, int DK>
@@ -964,16 +963,15 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
 {
     typedef typename X::E E;
     typedef typename X::Exact Exact;
-    typedef typename X::Pair Pair;
     typedef typename X::Split Split;
     typedef Lds<X, DK> L;
     typedef GradLds<X, DK> G;
     constexpr int kWide = G::kWide, kTok = L::kTok, TI = DK / 32;       // TI: 16-token tiles of a wavefront
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     float *eG = reinterpret_cast<float *>(lds_raw), *eEnd = eG + C, *bs = eEnd + C, *hi_of = bs + C, *lo_of = hi_of + C, *qd = lo_of + C, *vd = qd + 8 * C, *part = vd + C;
-    E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPairPlanes * C * kWide;
-    E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPairPlanes * L::kSquare;
-    float *kd = reinterpret_cast<float *>(Es + X::kPairPlanes * L::kSquare);        // k.X of eight wavefronts
+    E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPlanes * C * kWide;
+    E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPlanes * L::kSquare;
+    float *kd = reinterpret_cast<float *>(Es + X::kPlanes * L::kSquare);        // k.X of eight wavefronts
     const Sizes &z = a.z;
     const int wave = wave_index();
     int tid = threadIdx.x;
@@ -1057,8 +1055,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         for (int half = 0; half < 2; ++half) {
             const int i = (tid >> 4) + 32 * half;
             fence();
-            Split us;
-            Pair rs;
+            Split us, rs;
             split8(u[half], us);
             split8(r[half], rs);
             put8(Us + i * kWide + p0, C * kWide, us);
@@ -1105,7 +1102,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                     get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
                     jobs[k] = mma(u, tokens_o(16 * ti, p), jobs[k]);
                 } else {
-                    Pair u, r;
+                    Split u, r;
                     get8(Us + (16 * tj + col) * kWide + p + 8 * q, C * kWide, u);
                     get8(Rs + (16 * ti + col) * kWide + p + 8 * q, C * kWide, r);
                     jobs[k] = mma(u, r, jobs[k]);
@@ -1121,11 +1118,10 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
             if (kb >= deep) continue;
             const int p = 32 * kb;
             fence();
-            Split ss;
-            Pair ds;
+            Split ss, ds;
             split8(s[kb], ss);
             split8(d[kb], ds);
-            Pair u[2], r[2];
+            Split u[2], r[2];
             Exact o[2];
             auto get = [&](int t) {
                 const int row = 16 * (ti0 + t);
@@ -1140,7 +1136,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 else if (t + 1 < TI) get(t + 1);
                 fence();
                 dq[t] = mma(o[t & 1], ss, dq[t]);
-                y[t] = mma(r[t & 1], lead(ss), y[t]);
+                y[t] = mma(r[t & 1], ss, y[t]);
                 dk[t] = mma(u[t & 1], ds, dk[t]);
                 if (kNext) fence();
             }
@@ -1183,18 +1179,18 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 for (int e = 0; e < 4; ++e) f0[e] = j0 + e <= i ? f[e] : 0.f;
                 put4(F + i * kTok + spread(j0), L::kSquare, f0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) put1_pair(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
+                for (int e = 0; e < 4; ++e) put1(Ft + (j0 + e) * kTok + spread(i), L::kSquare, f0[e]);
             } else {
                 const bool idle_i = bs[i] == 0.f;
                 const f32x4 x = (idle_i ? -1.f : -bs[i]) * D * jobs[k];
                 f32x4 x0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x0[e] = j0 + e < i ? x[e] : 0.f;
-                put4_pair(Es + i * kTok + spread(j0), L::kSquare, x0);
+                put4(Es + i * kTok + spread(j0), L::kSquare, x0);
                 // after the rows: in a diagonal tile these places hold its zeros
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (j0 + e < i) put1_pair(Es + (j0 + e) * kTok + spread(i), L::kSquare, idle_i ? 0.f : x[e]);
+                    if (j0 + e < i) put1(Es + (j0 + e) * kTok + spread(i), L::kSquare, idle_i ? 0.f : x[e]);
             }
         }
         fence();
@@ -1205,7 +1201,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
             const int t = 2 * (wave & 1);
             E *to = wave < 6 ? F + (16 * t + col) * kTok + spread(16 * t + 16 + 4 * q) : Ft + (16 * t + 16 + col) * kTok + spread(16 * t + 4 * q);
             if (wave < 6) put4(to, L::kSquare, zero4());
-            else put4_pair(to, L::kSquare, zero4());
+            else put4(to, L::kSquare, zero4());
         }
         __syncthreads();
         // dQ += F K, dK += F^T Q + (E + E^T) K
@@ -1213,7 +1209,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         for (int kb = 0; kb < 2; ++kb) {
             const int p = 32 * kb + 8 * q;
             const Exact k = get8(Kt + dcol * kTok + p), qq = get8(Qt + dcol * kTok + p);
-            Pair e[2], ft[2];
+            Split e[2], ft[2];
             Split f[2];
             auto get = [&](int t) {
                 const int ti = ti0 + t, place = (16 * ti + col) * kTok + p;
@@ -1390,7 +1386,7 @@ template <class X, int DK>
 constexpr size_t scan_lds(bool out)
 {
     typedef Lds<X, DK> L;
-    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPlanes * L::kSquare + (out ? L::kByTokens + X::kPairPlanes * L::kSquare : 0)) + kDec * sizeof(float);
+    return sizeof(typename X::E) * (L::kByTokens + L::kByRows + X::kPlanes * L::kSquare + (out ? L::kByTokens + X::kPlanes * L::kSquare : 0)) + kDec * sizeof(float);
 }
 template <class X, int DK>
 constexpr size_t rev_lds()
