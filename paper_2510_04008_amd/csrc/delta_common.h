@@ -17,10 +17,11 @@
 //     dQ = F K + scale e^G dO S^T
 //     dK = F^T Q + (E + E^T) K + e^{G_C - G} U dS^T - b e^G dR S^T
 //     db_i = u_i.dR_i / b_i
-//     dG_i = q_i.dQ_i - v_i.dV_i,   dg_t = sum_{i >= t, in the chunk} dG_i + <S', dS>
-// The last line: with S_t = e^{G_t} Z_t the recurrence of Z holds no decay, only v_t e^{-G_t} and o_t e^{G_t} do, so the cotangent of
-// G_t is o_t.dO_t - v_t.dV_t, and o is linear in q; a chunk's sum starts from the inner product at its end, which
-// keeps rounding errors from adding up along the sequence.
+//     dg_t = sum_{j < t <= i} W_ij + sum_{i >= t} p_i + sum_{j < t} s_j + e^{G_C} <S, dS>,   over the chunk, with
+//         W_ij = M_ij dO_i.u_j - A_ij dR_i.u_j,   p_i = q_i.(scale e^{G_i} S dO_i) - k_i.(b_i e^{G_i} S dR_i),   s_j = k_j.(e^{G_C - G_j} dS u_j)
+// The last: e^{g_t} is a factor of what passes t and of nothing else, from a token before it (or the chunk's start) to one at or behind it (or the chunk's
+// end).  Every term of the sum holds that factor, so dg_t keeps its digits however small it is.  (The cotangent of G_i is q_i.dQ_i - v_i.dV_i, and dg
+// its sum from the end; but both of these hold terms without any decay, and with g = -8 their difference has lost 3 of 7 digits.)
 // Tokens of strength zero (padding; |b| below 2^-100 counts as that) write nothing, whatever finite values their rows hold: their rows of A and of
 // b (V - e^G K S) are zeros, not products with zero.  db divides by b; for them it is v_i.dR_i + k_i.X_i with
 //     X_i = -sum_j D_ij (dR_i.u_j) k_j - e^{G_i} S dR_i,

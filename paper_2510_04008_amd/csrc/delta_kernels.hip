@@ -44,7 +44,7 @@ __device__ __forceinline__ void kept8(const float *p, float *x)
 }
 
 // ------------------------------------------------------------------ what a chunk needs besides the states
-// T and the decays of one chunk of one head, and for the backward pass M^T.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane
+// T and the decays of one chunk of one head, and for the backward pass M^T, T^T and A^T.  T: the four 16 x 16 diagonal blocks by substitution (one wavefront, a lane
 // per column), then [[T1, 0], [-T2 A21 T1, T2]] twice on the fp32 matrix instructions, each block in A's place.  Substitution and not powers of A: with keys
 // alike the powers reach thousands where T stays near one.
 // Images are written in the order in which the scans' operands lie in LDS (rows in spread order), in fp32: half of the bytes of a Split.
@@ -90,7 +90,7 @@ struct PrepArgs {
     Sizes z;
     const void *Q, *K;
     const float *g, *beta;
-    float *T, *MT, *TT;     // 64 x 64 images, rows in spread order: T - I; backward also M^T and T^T - I
+    float *T, *MT, *TT, *AT;        // 64 x 64 images, rows in spread order: T - I; backward also M^T, T^T - I and, on and below A's diagonal, A^T
     float *dec;             // per chunk (kDec): e^G, e^{G_C - G}, beta, and G as the sum of two floats
 };
 
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
     }
     __syncthreads();
     if (wave < 3) {
-        float *MT = a.MT + at * C * C + (32 * tj + col) * C + 32 * ti;
+        const size_t to = at * C * C + (32 * tj + col) * C + 32 * ti;
         const int j = 32 * tj + col;
         const float hj = hi_of[j], lj = lo_of[j];
         const bool idle_j = B[j] == 0.f;
@@ -142,15 +142,18 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(PrepArgs a)
         for (int e4 = 0; e4 < 4; ++e4) {
             const int i0 = 32 * ti + acc_row(4 * e4, h);
             const f32x4 hi = *reinterpret_cast<const f32x4 *>(hi_of + i0), lo = *reinterpret_cast<const f32x4 *>(lo_of + i0), b = *reinterpret_cast<const f32x4 *>(B + i0);
-            f32x4 m;
+            f32x4 m, y4;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float D = decay(hi[e], lo[e], hj, lj), x = z.scale * D * qk[4 * e4 + e], y = b[e] * D * kk[4 * e4 + e];
                 m[e] = j <= i0 + e ? (idle_j ? idle(x) : x) : 0.f;
                 // (the column of a token of strength zero meets its zeros; only its own cotangent reads it)
-                A[i0 + e][j] = j < i0 + e && b[e] != 0.f ? (idle_j ? (BWD ? idle(y) : 0.f) : y) : 0.f;
+                A[i0 + e][j] = y4[e] = j < i0 + e && b[e] != 0.f ? (idle_j ? (BWD ? idle(y) : 0.f) : y) : 0.f;
             }
-            if (BWD) *reinterpret_cast<f32x4 *>(MT + spread(acc_row(4 * e4, h))) = m;
+            if (BWD) {
+                *reinterpret_cast<f32x4 *>(a.MT + to + spread(acc_row(4 * e4, h))) = m;
+                *reinterpret_cast<f32x4 *>(a.AT + to + spread(acc_row(4 * e4, h))) = y4;
+            }
         }
     }
     __syncthreads();
@@ -413,7 +416,7 @@ struct ScanArgs {
     void *O;
     float *P, *PT;                  // kPre: the transition and its transpose, per segment
     int transitions;                // kPre
-    float *S, *U;                   // kKeep: states at the chunks' starts and behind the last, and U, rows in spread order
+    float *S, *U;                   // kKeep: states at the chunks' starts, and U, rows in spread order
 };
 
 template <class X, int DK, int THREADS, int MODE>
@@ -522,7 +525,7 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         for (int kb = 0; kb < DK / 32; ++kb) {
             const Split s = operand<Split>(S[2 * kb], S[2 * kb + 1]);
             if (sizeof(E) == 4) fence();
-            if (MODE == kKeep) keep_state<X, DK>(a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c) * DK * z.dvp, 2 * kb, z.dvp, 16 * tile, s, lane);
+            if (MODE == kKeep) keep_state<X, DK>(a.S + at * DK * z.dvp, 2 * kb, z.dvp, 16 * tile, s, lane);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
                 R[ti] = mma(tile8<X, L::kRow>(Ks, 16 * ti, 32 * kb, lane), s, R[ti]);
@@ -587,11 +590,6 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
         }
     }
     if (!active) return;
-    if (MODE == kKeep && c1 == z.chunks) {
-        float *keep = a.S + (static_cast<size_t>(bh) * (z.chunks + 1) + c1) * DK * z.dvp;
-#pragma unroll
-        for (int t = 0; t < DK / 16; t += 2) keep_state<X, DK>(keep, t, z.dvp, 16 * tile, operand<Split>(S[t], S[t + 1]), lane);
-    }
     if (trans) {
         // P row by row; P^T: its columns, of which a lane holds eight rows that lie together
         float *P = a.P + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK, *PT = a.PT + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK;
@@ -899,7 +897,7 @@ __global__ __launch_bounds__(THREADS) void delta_rev_kernel(RevArgs a)
 struct GradArgs {
     Sizes z;
     const void *Q, *K, *V, *dO;
-    const float *dec, *S, *U, *dS, *dR;
+    const float *dec, *MT, *AT, *S, *U, *dS, *dR;
     void *dQ, *dK;                  // the caller's tensors, or with `shared` fp32 (BH, 64 chunks, dk) parts
     int shared;
     float *dg, *dbeta;
@@ -937,11 +935,35 @@ __device__ __forceinline__ float sum_lanes(float (&v)[N], int lane)
     fold_lanes<8>(v, lane);
     return v[0];
 }
+// within each 16 lanes: the value N lanes above (below with N < 0), zero beyond the ends; the sum over this lane and those above it; the sum over those below it
+template <int N>
+__device__ __forceinline__ float lanes_off(float x)
+{
+    constexpr int kRowShl = 0x100, kRowShr = 0x110;
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), N > 0 ? kRowShl + N : kRowShr - N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float suffix16(float x)
+{
+    x += lanes_off<1>(x);
+    x += lanes_off<2>(x);
+    x += lanes_off<4>(x);
+    return x + lanes_off<8>(x);
+}
+__device__ __forceinline__ float prefix16(float x)
+{
+    x = lanes_off<-1>(x);
+    x += lanes_off<-1>(x);
+    x += lanes_off<-2>(x);
+    x += lanes_off<-4>(x);
+    return x + lanes_off<-8>(x);
+}
 
 // One workgroup of eight wavefronts per chunk.  U, dR and dO are read once, into LDS, as operands; a wavefront then has 16 columns of dQ and dK
 // (and with dk <= 64 half of the tokens), for which it reads its rows of S and dS once, as right operands: dO S^T, dR S^T and U dS^T.  F and E are
 // formed from the same tiles before these are overwritten with F, F^T and E + E^T, whose products with K and Q end the kernel.  A workgroup goes on to the
-// chunk before it, whose states it has asked for by then; <S', dS> takes S' from the chunk behind.
+// chunk before it, whose states it has asked for by then.
+// dg: W = M o (dO U^T) - A o (dR U^T) lies in the same 16 x 16 tiles as F and E, rows j in registers and columns i in lanes.  A tile's sums over i >= t are four
+// steps over the lanes; below the diagonal they and the sums of its rows j are all that dg needs of it (kPairs), and one wavefront adds up a chunk's.
 // 4096 chunks of dk = dv = 128, bf16: 342 us for 288 KB a chunk, 3.5 TB/s.  LDS holds one workgroup of a CU, which waits for its own reading at the chunk's start
 // and for tiles in LDS after that.
 constexpr int kGradThreads = 512;
@@ -952,10 +974,12 @@ struct GradLds {
     typedef Lds<X, DK> L;
     static constexpr int kWide = 128 + X::kPad;                         // a token's row over columns of the state, in spread order
     static constexpr bool kHasO = sizeof(E) == 2;                       // dO has no room beside fp32 tiles: its operands come from memory
-    static constexpr int kFloats = kDec + 8 * C + C + 8;                // decays and strengths, q.dq of eight wavefronts, v.dv, partial sums
+    static constexpr int kPairs = 20 * 32;                              // of a tile of W's two products: sums over i >= t and j, and over i for each j
+    static constexpr int kFloats = kDec + kPairs + C + 8;               // decays and strengths, sums of W, v.dR, partial sums
+    static constexpr int kDots = 3 * 8 * C;                             // p, s and k.X of eight wavefronts
     static constexpr int kTiles = C * kWide * (2 * X::kPlanes + (kHasO ? 1 : 0));
     static constexpr size_t kBytes = kFloats * sizeof(float) + sizeof(E) * (2 * L::kByRows + kTiles);
-    static_assert(3 * X::kPlanes * L::kSquare * sizeof(E) + 8 * C * sizeof(float) <= kTiles * sizeof(E), "F, F^T, E + E^T and k.X lie where U, dR and dO were");
+    static_assert(3 * X::kPlanes * L::kSquare * sizeof(E) + kDots * sizeof(float) <= kTiles * sizeof(E), "F, F^T, E + E^T and these sums lie where U, dR and dO were");
 };
 
 template <class X, int DK>
@@ -968,16 +992,15 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
     typedef GradLds<X, DK> G;
     constexpr int kWide = G::kWide, kTok = L::kTok, TI = DK / 32;       // TI: 16-token tiles of a wavefront
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    float *eG = reinterpret_cast<float *>(lds_raw), *eEnd = eG + C, *bs = eEnd + C, *hi_of = bs + C, *lo_of = hi_of + C, *qd = lo_of + C, *vd = qd + 8 * C, *part = vd + C;
+    float *eG = reinterpret_cast<float *>(lds_raw), *eEnd = eG + C, *bs = eEnd + C, *hi_of = bs + C, *lo_of = hi_of + C, *pairs = lo_of + C, *vd = pairs + G::kPairs, *part = vd + C;
     E *Kt = reinterpret_cast<E *>(part + 8), *Qt = Kt + L::kByRows, *Us = Qt + L::kByRows, *Rs = Us + X::kPlanes * C * kWide, *Os = Rs + X::kPlanes * C * kWide;
     E *F = Us, *Ft = F + X::kPlanes * L::kSquare, *Es = Ft + X::kPlanes * L::kSquare;
-    float *kd = reinterpret_cast<float *>(Es + X::kPlanes * L::kSquare);        // k.X of eight wavefronts
+    float *pd = reinterpret_cast<float *>(Es + X::kPlanes * L::kSquare), *sd = pd + 8 * C, *kd = sd + 8 * C;
     const Sizes &z = a.z;
     const int wave = wave_index();
     int tid = threadIdx.x;
     int lane = tid & 63, q = lane >> 4, col = lane & 15;
     const int bh = blockIdx.y, c_low = blockIdx.x * a.each, c_high = min(c_low + a.each, z.chunks);
-    const float *S0 = a.S + static_cast<size_t>(bh) * (z.chunks + 1) * DK * z.dvp;
     const int deep = z.dvp / 32;            // steps of a product over the state's columns
     int dcol = 16 * (wave % (DK / 16)) + col;
     const int ti0 = DK == 128 ? 0 : wave / (DK / 16) * TI;
@@ -985,7 +1008,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
 
     // what a chunk reads: asked for at once, and while the products of the chunk before are formed
     RowsStage<X, DK> rows;
-    float u[2][8], r[2][8], s[4][8], d[4][8], s1[4][8], decs = 0.f;
+    float u[2][8], r[2][8], s[4][8], d[4][8], decs = 0.f;
+    f32x4 ma[3];                    // of M and A, what the wavefront's tiles of F and E are multiplied with
     Exact v[2], o[2];
     auto take_state = [&](const float *from, float (&to)[4][8]) {
 #pragma unroll
@@ -1019,12 +1043,21 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
             v[half] = rows8_spread<X>(static_cast<const E *>(a.V) + row0 * z.dv, i, p0 < z.dvp ? n : 0, z.dv, p0);
             o[half] = rows8_spread<X>(static_cast<const E *>(a.dO) + row0 * z.dv, i, p0 < z.dvp ? n : 0, z.dv, p0);
         }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int job = wave + 8 * k, t = job < 10 ? job : job - 10;
+            if (job >= 20) continue;
+            const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
+            const float *from = (job < 10 ? a.MT : a.AT) + at * C * C + (16 * tj + 4 * q) * C + spread(16 * ti + col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ma[k][e] = from[e * C];
+        }
     };
     auto take_states = [&](int c) {
-        take_state(S0 + static_cast<size_t>(c) * DK * z.dvp, s);
-        take_state(a.dS + (static_cast<size_t>(bh) * z.chunks + c) * DK * z.dvp, d);
+        const size_t at = static_cast<size_t>(bh) * z.chunks + c;
+        take_state(a.S + at * DK * z.dvp, s);
+        take_state(a.dS + at * DK * z.dvp, d);
     };
-    take_state(S0 + static_cast<size_t>(c_high) * DK * z.dvp, s1);
     if (c_low < c_high) take_states(c_high - 1);
     for (int c = c_high - 1; c >= c_low; --c) {
         // (what follows from the lane is formed anew for each chunk, not kept in registers)
@@ -1039,17 +1072,16 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         take(c);
         __syncthreads();                        // the chunk before is done with the tiles
         if (tid < kDec) eG[tid] = decs;
-        for (int i = tid; i < 8 * C; i += kGradThreads) qd[i] = 0.f;
         if (has_k || has_q) rows.template put<false, true, false>(n, z.dk, nullptr, has_k ? Kt : Qt, task);
         __syncthreads();                        // the strengths
         const bool idle_tokens = __any(lane < n && bs[lane] == 0.f);
-        // the tiles, and on the way u.dR and v.dR of every token; over the states <S', dS>
+        // the tiles, and on the way u.dR and v.dR of every token; over the states <S, dS>
         float dot = 0.f;
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
             if (kb < deep) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot += s1[kb][e] * d[kb][e];
+                for (int e = 0; e < 8; ++e) dot += s[kb][e] * d[kb][e];
             }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -1108,6 +1140,19 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                     jobs[k] = mma(u, r, jobs[k]);
                 }
             }
+            // the tile of W: sums over i' >= i, of them those over j < i and, below the diagonal, the whole rows j
+            f32x4 w;
+            float over_j = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = job < 10 ? ma[k][e] * jobs[k][e] : -ma[k][e] * jobs[k][e];
+                w[e] = suffix16(ti > tj || 4 * q + e < col ? w[e] : 0.f);
+                over_j += ti > tj || 4 * q + e < col ? w[e] : 0.f;
+            }
+            over_j += __shfl_xor(over_j, 16);
+            over_j += __shfl_xor(over_j, 32);
+            if (q == 0) pairs[32 * job + col] = over_j;
+            if (col == 0) *reinterpret_cast<f32x4 *>(pairs + 32 * job + 16 + 4 * q) = w;
         }
         // dQ = scale e^G dO S^T, and of dK: e^{G_C - G} U dS^T - b e^G dR S^T (b = 0: X's part)
         f32x4 dq[TI], dk[TI], y[TI];
@@ -1141,24 +1186,31 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 if (kNext) fence();
             }
         }
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s1[kb][e] = s[kb][e];
         if (ti0 > 0) dot = 0.f;         // with dk <= 64 two wavefronts have met the same rows
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) dot += __shfl_xor(dot, m);
         if (lane == 0) part[wave] = dot;
+        // p, s (and further down k.X): sums over the wavefront's columns, of which a lane has one token's
+        float ps[4 * TI], ss[4 * TI];
 #pragma unroll
         for (int t = 0; t < TI; ++t) {
             const int i = 16 * (ti0 + t) + 4 * q;
             const f32x4 g = *reinterpret_cast<const f32x4 *>(eG + i), b = *reinterpret_cast<const f32x4 *>(bs + i);
-            f32x4 b1;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) b1[e] = b[e] != 0.f ? b[e] : 1.f;
+            float xq[4], xk[4];
+            get4(Qt + dcol * kTok + spread(i), xq);
+            get4(Kt + dcol * kTok + spread(i), xk);
             dq[t] *= z.scale * g;
-            dk[t] = *reinterpret_cast<const f32x4 *>(eEnd + i) * dk[t] - b1 * g * y[t];
+            dk[t] *= *reinterpret_cast<const f32x4 *>(eEnd + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float gy = g[e] * y[t][e];
+                ps[4 * t + e] = xq[e] * dq[t][e] - xk[e] * (b[e] * gy);
+                ss[4 * t + e] = xk[e] * dk[t][e];
+                dk[t][e] -= (b[e] != 0.f ? b[e] : 1.f) * gy;
+            }
         }
+        const float p_sum = sum_lanes(ps, lane), s_sum = sum_lanes(ss, lane);
+        const int sum_at = wave * C + 16 * (ti0 + (col % (4 * TI) >> 2)) + 4 * q + (col & 3);
         __syncthreads();
         // F, its transpose, and E + E^T (b = 0: the row of X, and nothing in E^T)
 #pragma unroll
@@ -1193,6 +1245,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                     if (j0 + e < i) put1(Es + (j0 + e) * kTok + spread(i), L::kSquare, idle_i ? 0.f : x[e]);
             }
         }
+        if (col < 4 * TI) pd[sum_at] = p_sum, sd[sum_at] = s_sum;
         fence();
         if (c > c_low) take_states(c - 1);
         fence();
@@ -1230,29 +1283,22 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
                 if (kNext) fence();
             }
         }
-        // a row's elements times those of a gradient, summed over the wavefront's columns
-        auto row_dots = [&](const E *rows, const f32x4 (&grad)[TI], float *to) {
-            float v[4 * TI];
-#pragma unroll
-            for (int t = 0; t < TI; ++t) {
-                float x[4];
-                get4(rows + dcol * kTok + spread(16 * (ti0 + t) + 4 * q), x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * t + e] = x[e] * grad[t][e];
-            }
-            const float s = sum_lanes(v, lane);
-            const int w = col % (4 * TI);
-            if (col < 4 * TI) to[wave * C + 16 * (ti0 + (w >> 2)) + 4 * q + (w & 3)] = s;
-        };
-        row_dots(Qt, dq, qd);
         if (idle_tokens) {
-            row_dots(Kt, dk, kd);
+            float ks[4 * TI];
 #pragma unroll
             for (int t = 0; t < TI; ++t) {
-                const f32x4 b = *reinterpret_cast<const f32x4 *>(bs + 16 * (ti0 + t) + 4 * q);
+                const int i = 16 * (ti0 + t) + 4 * q;
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(bs + i);
+                float x[4];
+                get4(Kt + dcol * kTok + spread(i), x);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dk[t][e] = b[e] != 0.f ? dk[t][e] : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    ks[4 * t + e] = x[e] * dk[t][e];
+                    dk[t][e] = b[e] != 0.f ? dk[t][e] : 0.f;
+                }
             }
+            const float k_sum = sum_lanes(ks, lane);
+            if (col < 4 * TI) kd[sum_at] = k_sum;
         }
         const int d0 = dcol - col;
         if (a.shared) {
@@ -1276,27 +1322,41 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(GradArgs a)
         }
         __syncthreads();
         if (wave == 0) {
-            const bool idle_token = bs[lane] == 0.f;
-            float mine = idle_token ? 0.f : -bs[lane] * vd[lane], tail = 0.f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                mine += qd[w * C + lane];
-                tail += part[w];
-            }
-            if (idle_token && lane < n) {
-                float b = vd[lane];
+            auto over_wavefronts = [&](const float *x) {
+                float s = 0.f;
 #pragma unroll
                 for (int w = 0; w < 8; ++w)
-                    if (DK == 128 || w / (DK / 16) == lane / 32) b += kd[w * C + lane];       // (with dk <= 64 a wavefront has half of the tokens)
-                a.dbeta[row0 + lane] = b;
+                    if (DK == 128 || w / (DK / 16) == lane / 32) s += x[w * C + lane];       // (with dk <= 64 a wavefront has half of the tokens)
+                return s;
+            };
+            // across the token's tile of 16: from tiles before it, to tiles behind it, within it, and past the whole of it
+            float sum = 0.f, rows_j = 0.f;
+            const int x = lane >> 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int ti = max(x, k), tile = 32 * (ti * (ti + 1) / 2 + min(x, k));
+                if (k <= x) sum += pairs[tile + col] + pairs[tile + 320 + col];
+                else rows_j += pairs[tile + 16 + col] + pairs[tile + 336 + col];
             }
-            float s = mine;         // sum over this token and those behind it
+            sum += prefix16(rows_j);
+            // (the first of a tile's sums over i' >= i is the whole tile's: of tiles 3 = (2, 0), 6 = (3, 0), 7 = (3, 1))
+            const float past20 = pairs[96] + pairs[416], past30 = pairs[192] + pairs[512], past31 = pairs[224] + pairs[544];
+            if (x == 1) sum += past20 + past30;
+            if (x == 2) sum += past30 + past31;
+            float tail = 0.f, p = over_wavefronts(pd), s = __shfl_up(over_wavefronts(sd), 1);
+            s = lane > 0 ? s : 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) tail += part[w];
+            // p of this token and those behind it, s of those before it
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const float y = __shfl_down(s, d);
-                if (lane + d < 64) s += y;
+                const float y = __shfl_down(p, d), z = __shfl_up(s, d);
+                if (lane + d < 64) p += y;
+                if (lane >= d) s += z;
             }
-            if (lane < n) a.dg[row0 + lane] = s + tail;
+            s += p + sum + eG[C - 1] * tail;
+            if (lane < n && bs[lane] == 0.f) a.dbeta[row0 + lane] = vd[lane] + over_wavefronts(kd);
+            if (lane < n) a.dg[row0 + lane] = s;
         }
     }
 }
@@ -1431,7 +1491,8 @@ struct Passes {
     static constexpr int kTiles = THREADS / 64;
     static hipError_t prep(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, bool bwd, hipStream_t st)
     {
-        PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr, floats(ws, p.off_dec)};
+        PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr,
+                   bwd ? floats(ws, p.off_AT) : nullptr, floats(ws, p.off_dec)};
         const dim3 grid(z.chunks, p.BH);
         if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
         else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
@@ -1629,7 +1690,7 @@ struct Passes {
             }
             const float *a_S = floats(ws, p.off_S), *a_U = floats(ws, p.off_U);
             const bool shared = p.H != p.Hk;
-            GradArgs g{z, io.Q, io.K, io.V, io.dO, r.dec, a_S, a_U, full.dS, full.dR,
+            GradArgs g{z, io.Q, io.K, io.V, io.dO, r.dec, r.MT, floats(ws, p.off_AT), a_S, a_U, full.dS, full.dR,
                        shared ? ws + p.off_pq : io.dQ, shared ? ws + p.off_pk : io.dK, shared ? 1 : 0, io.dg, io.dbeta,
                        std::max(1, (z.chunks * p.BH + 255) / 256)};
             DELTA_LAUNCH("delta_gradients", (delta_grad_kernel<X, DK>), dim3((z.chunks + g.each - 1) / g.each, p.BH), kGradThreads, (GradLds<X, DK>::kBytes), st, g);

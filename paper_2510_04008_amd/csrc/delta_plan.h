@@ -18,8 +18,8 @@ struct DeltaPlan {
     int chunks;                     // of 64 tokens
     int seg_chunks, nseg;           // chunks per segment (the last may be short), segments
     int win_segs, windows;          // segments per window (the last may hold fewer), windows: a window's workspace is the next one's too
-    // workspace, byte offsets (multiples of 256).  Per window: T, decays and, backward, M^T, T^T, states, U, cotangents, dR
-    size_t off_T, off_dec, off_MT, off_TT, off_S, off_U, off_dS, off_dR, off_pq, off_pk;
+    // workspace, byte offsets (multiples of 256).  Per window: T, decays and, backward, M^T, T^T, A^T, states, U, cotangents, dR
+    size_t off_T, off_dec, off_MT, off_TT, off_AT, off_S, off_U, off_dS, off_dR, off_pq, off_pk;
     // per segment of the sequence: states (cotangents) from zero, transitions, states at the starts, cotangents at the ends
     size_t off_add, off_P, off_PT, off_start, off_end;
     int join_groups;                // at most, of a window's segments (delta_combine_kernel); their transitions, states from zero and starts

@@ -78,7 +78,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         return RACE_OK;
     }
     const size_t dkp = d->dk <= 64 ? 64 : 128, one = sizeof(float) * p.dk * p.dv, square = kChunk * kChunk;
-    const size_t per_chunk = square * 4 + 5 * kChunk * 4 + (backward ? square * 8 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
+    const size_t per_chunk = square * 4 + 5 * kChunk * 4 + (backward ? square * 12 + 8 * p.dvp * (dkp + kChunk) + (p.H != p.Hk ? 8 * kChunk * p.dk : 0) : 0);
     const int window = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.chunks, kWindowBytes / (per_chunk * p.BH))));
     if (d->chunk > 0) {
         p.seg_chunks = static_cast<int>((std::min(d->chunk, d->N) + kChunk - 1) / kChunk);
@@ -118,7 +118,8 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         if (p.win_segs > 1) p.off_end = take(segs * one);
         p.off_MT = take(n * square * 4);
         p.off_TT = take(n * square * 4);
-        p.off_S = take((n + p.BH) * dkp * p.dvp * 4);
+        p.off_AT = take(n * square * 4);
+        p.off_S = take(n * dkp * p.dvp * 4);
         p.off_U = take(n * kChunk * p.dvp * 4);
         p.off_dS = take(n * dkp * p.dvp * 4);
         p.off_dR = take(n * kChunk * p.dvp * 4);
