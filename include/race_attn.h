@@ -246,7 +246,10 @@ typedef struct {
     int64_t chunk;    /* tokens per scan segment, rounded up to whole chunks; 0 = choose                */
 } race_delta_desc_t;
 
-/* Bytes of device workspace of race_delta_fwd and of race_delta_bwd.  0 for an invalid or unsupported descriptor and for N == 0. */
+/* Bytes of device workspace of race_delta_fwd and of race_delta_bwd.  0 for an invalid or unsupported descriptor and for N == 0.
+ * A long sequence is worked on in windows of at most 4 GiB, which follow one another in the same memory, but no window is less than one segment of every head: with
+ * desc->chunk = N all of the sequence's chunks of 64 tokens are held at once (dk = dv = 128: 17 KB each, backward 0.26 MB, with shared heads 0.32 MB).  What is held of
+ * every segment of the sequence is one state a head, backward also its transition (dk = 128: 64 KB). */
 size_t race_delta_workspace_bytes(const race_delta_desc_t *desc);
 size_t race_delta_bwd_workspace_bytes(const race_delta_desc_t *desc);
 /* Bytes of one state (B, H, dk, dv are used); 0 for an invalid descriptor. */

@@ -16,7 +16,7 @@ struct Sizes {
     int64_t N;
     int H, Hk, dk, dv, dvp;         // dvp: dv rounded up to 32
     float scale;
-    int seg_chunks, nseg;           // chunks per segment, segments of the sequence
+    int seg_chunks, nseg, win_segs; // chunks per segment, segments of the sequence, of a window (the last may hold fewer)
     int seg0, segs;                 // the window: first segment, segments
     int chunk0, chunks;             // first chunk, chunks
 };
@@ -414,7 +414,7 @@ struct ScanArgs {
     float *final_state;             // state behind the window's last segment (null: not wanted); kPre: behind every segment
     size_t final_head;
     void *O;
-    float *P, *PT;                  // kPre: the transition and its transpose, per segment
+    float *P, *PT;                  // kPre: the transition, per segment of the window, and its transpose, per segment of the sequence (null: not wanted)
     int transitions;                // kPre
     float *S, *U;                   // kKeep: states at the chunks' starts, and U, rows in spread order
 };
@@ -592,14 +592,16 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
     if (!active) return;
     if (trans) {
         // P row by row; P^T: its columns, of which a lane holds eight rows that lie together
-        float *P = a.P + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK, *PT = a.PT + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK;
+        float *P = a.P + (static_cast<size_t>(bh) * z.win_segs + seg) * DK * DK, *PT = a.PT + (static_cast<size_t>(bh) * z.nseg + z.seg0 + seg) * DK * DK;
         const int k0 = 16 * tile - z.dvp;
 #pragma unroll
         for (int t = 0; t < DK / 16; t += 2) {
             const Split x = operand<Split>(S[t], S[t + 1]);
-            f32x4 *to = reinterpret_cast<f32x4 *>(PT + transition_place<DK>(k0 + col, 16 * t + 8 * q));
-            to[0] = S[t];
-            to[1] = S[t + 1];
+            if (a.PT) {
+                f32x4 *to = reinterpret_cast<f32x4 *>(PT + transition_place<DK>(k0 + col, 16 * t + 8 * q));
+                to[0] = S[t];
+                to[1] = S[t + 1];
+            }
 #pragma unroll
             for (int b = 0; b < 2; ++b)
                 *reinterpret_cast<f32x4 *>(P + transition_place<DK>(16 * t + 16 * b + col, k0 + 4 * q)) = mma(x, unit8<X, false>(b, lane), zero4());
@@ -619,11 +621,10 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 struct CombineArgs {
     Sizes z;
     int heads, groups, each;        // transitions of a group: each; the last group's may be fewer
-    int steps;                      // transitions in all: segments first, first + 1, .. (REV: first, first - 1, ..)
+    int steps;                      // transitions in all: segments first, first + 1, .. of the window (REV: first, first - 1, ..)
     int first;
-    const float *P;                 // P_s: image bh * p_head + s; B_s: add + (bh * p_head + s) * dk * dv
-    size_t p_head;
-    const float *add;
+    const float *P, *add;           // P_s: image bh * p_head + s; B_s: add + (bh * add_head + s) * dk * dv
+    size_t p_head, add_head;
     const float *carry;             // state to start from (null: zero): carry + bh * carry_head + group * carry_group
     size_t carry_head, carry_group;
     float *at;                      // states at the segments' starts (REV: cotangents at their ends): at + bh * at_head + s * dk * dv; null: not wanted
@@ -667,13 +668,12 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
         for (int n = 0; n < COLS; ++n) put_state(reinterpret_cast<f32x4 (&)[1]>(S[n]), state, z.dk, z.dv, wave, col0 + 16 * n, lane);
     };
     auto take = [&](int i, Step &to) {
-        const size_t s = static_cast<size_t>(bh) * a.p_head + segment(i);
-        const float *p = a.P + s * DK * DK + wave * (DK / 32) * kOperand + lane * 8;
+        const float *p = a.P + (bh * a.p_head + segment(i)) * DK * DK + wave * (DK / 32) * kOperand + lane * 8;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) kept8(p + kb * kOperand, to.P[kb]);
 #pragma unroll
         for (int n = 0; n < COLS; ++n) to.B[n] = zero4();
-        if (!trans) get(to.B, a.add + s * one);
+        if (!trans) get(to.B, a.add + (bh * a.add_head + segment(i)) * one);
     };
     auto put = [&](int i) {
         if (a.at) put_to(a.at + bh * a.at_head + segment(i) * one);
@@ -1468,6 +1468,7 @@ Sizes sizes_of(const DeltaPlan &p)
     z.scale = p.scale;
     z.seg_chunks = p.seg_chunks;
     z.nseg = p.nseg;
+    z.win_segs = p.win_segs;
     return z;
 }
 void set_window(const DeltaPlan &p, int w, Sizes *z)
@@ -1510,16 +1511,16 @@ struct Passes {
         return a;
     }
     // transitions and states from zero of `segs` segments of the window
-    static hipError_t pre(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, int segs, hipStream_t st)
+    static hipError_t pre(const DeltaPlan &p, const Sizes &z, const DeltaIo &io, char *ws, int segs, bool bwd, hipStream_t st)
     {
         if (segs <= 0) return hipSuccess;
         ScanArgs a = scan_args(p, z, io, ws);
         const size_t one = static_cast<size_t>(p.dk) * p.dv;
-        a.final_state = floats(ws, p.off_add) + z.seg0 * one;
-        a.final_head = one * p.nseg;
+        a.final_state = floats(ws, p.off_add);
+        a.final_head = one * p.win_segs;
         a.transitions = 1;
         a.P = floats(ws, p.off_P);
-        a.PT = floats(ws, p.off_PT);
+        a.PT = bwd ? floats(ws, p.off_PT) : nullptr;
         const dim3 grid((p.dvp / 16 + DK / 16 + kTiles - 1) / kTiles, segs, p.BH);
         DELTA_LAUNCH("delta_segments", (delta_scan_kernel<X, DK, THREADS, kPre>), grid, THREADS, (scan_lds<X, DK>(false)), st, a);
         return hipSuccess;
@@ -1533,14 +1534,15 @@ struct Passes {
         a.heads = p.BH;
         a.groups = 1;
         a.each = a.steps = steps;
-        a.first = rev ? z.seg0 + z.segs - 1 : z.seg0;
-        a.P = floats(ws, rev ? p.off_PT : p.off_P);
-        a.p_head = p.nseg;
+        a.first = rev ? z.segs - 1 : 0;
+        a.P = rev ? floats(ws, p.off_PT) + static_cast<size_t>(z.seg0) * DK * DK : floats(ws, p.off_P);
+        a.p_head = rev ? p.nseg : p.win_segs;
         a.add = floats(ws, p.off_add);
+        a.add_head = p.win_segs;
         a.carry = carry;
         a.carry_head = carry_head;
-        a.at = floats(ws, rev ? p.off_end : p.off_start);
-        a.at_head = one * (rev ? p.nseg : p.nseg + 1);
+        a.at = rev ? floats(ws, p.off_end) : floats(ws, p.off_start) + z.seg0 * one;
+        a.at_head = one * (rev ? p.win_segs : p.nseg + 1);
         if (p.join_groups > 1 && steps >= kJoinInGroups) {
             const int each = (steps + p.join_groups - 1) / p.join_groups, groups = (steps + each - 1) / each;
             // the groups' transitions; the last group's is nobody's
@@ -1557,7 +1559,7 @@ struct Passes {
             g.steps = g.each = groups - 1;
             g.first = 0;
             g.P = c.out_P;
-            g.p_head = p.join_groups;
+            g.p_head = g.add_head = p.join_groups;
             g.add = c.out_add;
             g.at = floats(ws, p.off_group_start);
             g.at_head = one * p.join_groups;
@@ -1598,7 +1600,7 @@ struct Passes {
             a.start = carry;
             a.start_head = one;
             if (z.segs > 1) {
-                if (hipError_t e = pre(p, z, io, ws, z.segs - 1, st); e != hipSuccess) return e;
+                if (hipError_t e = pre(p, z, io, ws, z.segs - 1, false, st); e != hipSuccess) return e;
                 if (hipError_t e = combine(p, z, carry, one, ws, z.segs - 1, false, st); e != hipSuccess) return e;
                 a.start = floats(ws, p.off_start) + z.seg0 * one;
                 a.start_head = one * (p.nseg + 1);
@@ -1616,7 +1618,7 @@ struct Passes {
     {
         Sizes z = sizes_of(p);
         const size_t one = static_cast<size_t>(p.dk) * p.dv;
-        float *start = floats(ws, p.off_start), *end = floats(ws, p.off_end);
+        float *start = floats(ws, p.off_start);
         const bool joined = p.win_segs > 1;
         // states at the segments' starts
         const float *carry = io.state_in;
@@ -1624,7 +1626,7 @@ struct Passes {
             set_window(p, w, &z);
             if (hipError_t e = prep(p, z, io, ws, true, st); e != hipSuccess) return e;
             if (joined) {
-                if (hipError_t e = pre(p, z, io, ws, z.segs, st); e != hipSuccess) return e;
+                if (hipError_t e = pre(p, z, io, ws, z.segs, true, st); e != hipSuccess) return e;
                 // the windows' starts follow one another in `start`, so the next window's carry is read there
                 if (hipError_t e = combine(p, z, w == 0 ? io.state_in : start + z.seg0 * one, w == 0 ? one : one * (p.nseg + 1), ws, z.segs, false, st); e != hipSuccess)
                     return e;
@@ -1669,14 +1671,14 @@ struct Passes {
             full.end = dcarry;
             full.end_head = one;
             if (z.segs > 1) {
-                r.final_state = floats(ws, p.off_add) + z.seg0 * one;
-                r.final_head = one * p.nseg;
+                r.final_state = floats(ws, p.off_add);
+                r.final_head = one * p.win_segs;
                 r.seg_skip = 1;
                 const dim3 grid((p.dvp / 16 + kTiles - 1) / kTiles, z.segs - 1, p.BH);
                 DELTA_LAUNCH("delta_segments_back", (delta_rev_kernel<X, DK, THREADS, false>), grid, THREADS, (rev_lds<X, DK>()), st, r);
                 if (hipError_t e = combine(p, z, dcarry, one, ws, z.segs - 1, true, st); e != hipSuccess) return e;
-                full.end = end + z.seg0 * one;
-                full.end_head = one * p.nseg;
+                full.end = floats(ws, p.off_end);
+                full.end_head = one * p.win_segs;
             }
             full.final_state = w > 0 ? kept : io.dstate_in;
             full.final_head = one;

@@ -18,10 +18,11 @@ struct DeltaPlan {
     int chunks;                     // of 64 tokens
     int seg_chunks, nseg;           // chunks per segment (the last may be short), segments
     int win_segs, windows;          // segments per window (the last may hold fewer), windows: a window's workspace is the next one's too
-    // workspace, byte offsets (multiples of 256).  Per window: T, decays and, backward, M^T, T^T, A^T, states, U, cotangents, dR
+    // workspace, byte offsets (multiples of 256).  Per chunk of a window: T, decays and, backward, M^T, T^T, A^T, states, U, cotangents, dR
     size_t off_T, off_dec, off_MT, off_TT, off_AT, off_S, off_U, off_dS, off_dR, off_pq, off_pk;
-    // per segment of the sequence: states (cotangents) from zero, transitions, states at the starts, cotangents at the ends
-    size_t off_add, off_P, off_PT, off_start, off_end;
+    // per segment of a window: states (cotangents) from zero, transitions and, backward, cotangents at the ends; per segment of the sequence: states at the
+    // starts and, backward, transposed transitions (the windows are gone through from the last to the first once all starts are known)
+    size_t off_add, off_P, off_end, off_start, off_PT;
     int join_groups;                // at most, of a window's segments (delta_combine_kernel); their transitions, states from zero and starts
     size_t off_group_P, off_group_add, off_group_start;
     size_t off_carry;               // one state a head between windows

@@ -26,7 +26,8 @@ race_status_t check_workspace(const void *ws, size_t bytes, size_t need)
 }
 
 // ---------------------------------------------------------------- gated delta rule
-// What a window's chunks may take of the workspace.
+// What a window's chunks may take of the workspace.  A window holds a segment of every head at least, so a caller's segment length, or more heads than this holds
+// chunks of, take more.
 constexpr size_t kWindowBytes = size_t(4) << 30;
 
 race_status_t check_delta(const race_delta_desc_t *d)
@@ -100,11 +101,10 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
     };
     p.off_T = take(n * square * 4);
     p.off_dec = take(n * 5 * kChunk * sizeof(float));
-    const size_t segs = static_cast<size_t>(p.BH) * p.nseg;
+    const size_t segs = static_cast<size_t>(p.BH) * p.win_segs;
     if (p.win_segs > 1) {
         p.off_add = take(segs * one);
         p.off_P = take(segs * dkp * dkp * 4);
-        p.off_PT = take(segs * dkp * dkp * 4);
     }
     if (p.win_segs > kJoinInGroups) {
         p.join_groups = static_cast<int>(std::lround(std::sqrt(static_cast<double>(p.win_segs))));
@@ -112,10 +112,13 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         p.off_group_add = take(static_cast<size_t>(p.BH) * p.join_groups * one);
         p.off_group_start = take(static_cast<size_t>(p.BH) * p.join_groups * one);
     }
-    if (p.nseg > 1) p.off_start = take((segs + p.BH) * one);
+    if (p.nseg > 1) p.off_start = take(static_cast<size_t>(p.BH) * (p.nseg + 1) * one);
     if (p.windows > 1) p.off_carry = take(p.BH * one);
     if (backward) {
-        if (p.win_segs > 1) p.off_end = take(segs * one);
+        if (p.win_segs > 1) {
+            p.off_PT = take(static_cast<size_t>(p.BH) * p.nseg * dkp * dkp * 4);
+            p.off_end = take(segs * one);
+        }
         p.off_MT = take(n * square * 4);
         p.off_TT = take(n * square * 4);
         p.off_AT = take(n * square * 4);
