@@ -1495,7 +1495,7 @@ struct Passes {
         PrepArgs a{z, io.Q, io.K, io.g, io.beta, floats(ws, p.off_T), bwd ? floats(ws, p.off_MT) : nullptr, bwd ? floats(ws, p.off_TT) : nullptr,
                    bwd ? floats(ws, p.off_AT) : nullptr, floats(ws, p.off_dec)};
         const dim3 grid(z.chunks, p.BH);
-        if (bwd) DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
+        if (bwd) DELTA_LAUNCH("delta_prep_back", (delta_prep_kernel<X, DK, true>), grid, 256, 0, st, a);
         else DELTA_LAUNCH("delta_prep", (delta_prep_kernel<X, DK, false>), grid, 256, 0, st, a);
         return hipSuccess;
     }
@@ -1620,11 +1620,11 @@ struct Passes {
         const size_t one = static_cast<size_t>(p.dk) * p.dv;
         float *start = floats(ws, p.off_start);
         const bool joined = p.win_segs > 1;
-        // states at the segments' starts
+        // states at the segments' starts.  What the way back needs of a window's chunks is formed here for the last one alone, whose images stay.
         const float *carry = io.state_in;
         for (int w = 0; w < p.windows; ++w) {
             set_window(p, w, &z);
-            if (hipError_t e = prep(p, z, io, ws, true, st); e != hipSuccess) return e;
+            if (hipError_t e = prep(p, z, io, ws, w + 1 == p.windows, st); e != hipSuccess) return e;
             if (joined) {
                 if (hipError_t e = pre(p, z, io, ws, z.segs, true, st); e != hipSuccess) return e;
                 // the windows' starts follow one another in `start`, so the next window's carry is read there

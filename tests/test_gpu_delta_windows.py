@@ -74,3 +74,17 @@ def test_backward_beyond_two_to_the_31_elements():
                 _near(got[:, h:h + 1, tokens][:, :, mine], w[:, :, mine], n)
             if first:
                 _near(grads[5][:, h:h + 1], want[5], "dstate")
+
+
+def test_images_of_the_way_back_are_formed_once():
+    """A window's M^T, T^T and A^T: by the launch that its gradients read, not by the one before for its states alone."""
+    B, H, N, dk = 8, 128, 64 * 100 + 5, 8
+    x = _inputs(B, H, N, dk, dk, 0.05, seed=1)
+    d = ra.make_delta_desc(B, H, H, N, dk, dk, 0.3, ra.RACE_BF16, 256)
+    ra.race_attn_profile_enable(True)
+    ra.race_delta_bwd(d, *(x[n] for n in ("Q", "K", "V", "g", "beta")), x["dO"], state_in=x["state"])
+    torch.cuda.synchronize()
+    launches = {n: count for n, (_, count) in ra.race_attn_profile_read().items()}
+    ra.race_attn_profile_enable(False)
+    windows = launches["delta_scan_back"]
+    assert windows > 2 and launches["delta_prep_back"] == windows and launches["delta_prep"] == windows - 1
