@@ -292,7 +292,7 @@ typedef struct {
     int32_t neighbours;    /* 0: pairs (i, i + rot/2), 1: pairs (2i, 2i + 1)                                  */
     float eps;             /* >= 0, finite                                                                    */
     int32_t dtype;         /* race_dtype_t of rows, Q, K and their cotangents                                 */
-    int64_t pos0;          /* position of token 0 where positions is NULL                                     */
+    int64_t pos0;          /* position of token 0 where positions is NULL: pos0 + N up to 2^63 - 1            */
     int64_t q_strides[3], k_strides[3];    /* batch, token, head of the rows as given, elements, >= 0         */
     int64_t dq_strides[3], dk_strides[3];  /* the same of their cotangents (backward only): rows must not overlap */
 } race_rotary_desc_t;

@@ -167,10 +167,20 @@ race_status_t plan_rotary(const race_rotary_desc_t *d, rotary::RotaryPlan *pl)
     return RACE_OK;
 }
 
-// rows that would be written over one another
+struct Axis { int64_t n, stride; };
+// whether the last row, if there are any, ends within the bytes that 64 bits can count
+bool rows_in_range(const race_rotary_desc_t *d, int heads, const int64_t *s)
+{
+    if (heads == 0) return true;
+    int64_t reach = d->d, step;
+    for (const Axis &a : {Axis{d->B, s[0]}, Axis{d->N, s[1]}, Axis{heads, s[2]}})
+        if (a.n > 1 && (__builtin_mul_overflow(a.n - 1, a.stride, &step) || __builtin_add_overflow(reach, step, &reach))) return false;
+    return reach <= INT64_MAX / static_cast<int64_t>(sizeof(float));
+}
+// rows (in range) that would be written over one another
 bool rows_overlap(const race_rotary_desc_t *d, int heads, const int64_t *s)
 {
-    struct Axis { int64_t n, stride; } axes[3] = {{d->B, s[0]}, {d->N, s[1]}, {heads, s[2]}};
+    Axis axes[3] = {{d->B, s[0]}, {d->N, s[1]}, {heads, s[2]}};
     std::sort(axes, axes + 3, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
     int64_t reach = d->d;                   // elements from a row's first to behind the last that the axes so far can lead to
     for (const Axis &a : axes)
@@ -181,8 +191,9 @@ bool rows_overlap(const race_rotary_desc_t *d, int heads, const int64_t *s)
     return false;
 }
 
-race_status_t read_turns(const race_rotary_desc_t *d, const double *inv_freq, rotary::RotaryPlan *p)
+race_status_t read_turns(const race_rotary_desc_t *d, const double *inv_freq, const int64_t *positions, rotary::RotaryPlan *p)
 {
+    if (!positions && d->pos0 > INT64_MAX - d->N) return RACE_ERR_INVALID_ARG;
     if (d->rot > 0 && !inv_freq) return RACE_ERR_INVALID_ARG;
     for (int i = 0; i < d->rot / 2; ++i) {
         if (!std::isfinite(inv_freq[i])) return RACE_ERR_INVALID_ARG;
@@ -329,7 +340,8 @@ race_status_t race_qk_rotary_fwd(const race_rotary_desc_t *desc, const void *q, 
     if (s != RACE_OK) return s;
     if (p.N == 0) return RACE_OK;           // nothing to do, pointers may be null
     if (!q || !Q || (p.k.heads > 0 && (!k || !K))) return RACE_ERR_INVALID_ARG;
-    if ((s = read_turns(desc, inv_freq, &p)) != RACE_OK) return s;
+    if (!rows_in_range(desc, desc->Hq, desc->q_strides) || !rows_in_range(desc, desc->Hk, desc->k_strides)) return RACE_ERR_INVALID_ARG;
+    if ((s = read_turns(desc, inv_freq, positions, &p)) != RACE_OK) return s;
     if (any_equal({Q}, {q, k, wq, wk, positions, Q, K}) || (p.k.heads > 0 && any_equal({K}, {q, k, wq, wk, positions, Q, K}))) return RACE_ERR_INVALID_ARG;
     p.positions = positions;
     p.q.x = q, p.q.w = wq, p.q.y = Q;
@@ -347,6 +359,8 @@ race_status_t race_qk_rotary_bwd(const race_rotary_desc_t *desc, const void *q, 
     if (s != RACE_OK) return s;
     const bool keys = p.k.heads > 0;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (!rows_in_range(desc, desc->Hq, desc->q_strides) || !rows_in_range(desc, desc->Hk, desc->k_strides)) return RACE_ERR_INVALID_ARG;
+    if (!rows_in_range(desc, desc->Hq, desc->dq_strides) || !rows_in_range(desc, desc->Hk, desc->dk_strides)) return RACE_ERR_INVALID_ARG;
     if (rows_overlap(desc, desc->Hq, desc->dq_strides) || (keys && rows_overlap(desc, desc->Hk, desc->dk_strides))) return RACE_ERR_INVALID_ARG;
     if (p.N == 0) {                         // no rows, other pointers may be null; the sums over them are zero
         hipError_t e = dwq ? zero_floats(dwq, p.d, st) : hipSuccess;
@@ -354,7 +368,7 @@ race_status_t race_qk_rotary_bwd(const race_rotary_desc_t *desc, const void *q, 
         return e == hipSuccess ? RACE_OK : hip_failed(e, "race_qk_rotary_bwd launch");
     }
     if (!q || !dQ || !dq || (keys && (!k || !dK || !dk)) || (!keys && dwk)) return RACE_ERR_INVALID_ARG;
-    if ((s = read_turns(desc, inv_freq, &p)) != RACE_OK) return s;
+    if ((s = read_turns(desc, inv_freq, positions, &p)) != RACE_OK) return s;
     if (any_equal({dq}, {q, k, wq, wk, positions, dQ, dK, dq, dk, dwq, dwk}) || (keys && any_equal({dk}, {q, k, wq, wk, positions, dQ, dK, dq, dk, dwq, dwk})))
         return RACE_ERR_INVALID_ARG;
     if ((dwq && any_equal({dwq}, {q, k, wq, wk, positions, dQ, dK, dq, dk, dwq, dwk})) ||
