@@ -17,6 +17,8 @@ def _call(name, pos0=0, positions=False, B=3, Hk=2, **strides):
     place = p[11] if positions else None
     if name == "fwd":
         return ra.lib().race_qk_rotary_fwd(ctypes.byref(d), *p[:4], FREQ, place, p[4], p[5], None)
+    if Hk == 0:
+        p[9] = None
     # (a null workspace ends a call that is otherwise in order)
     return ra.lib().race_qk_rotary_bwd(ctypes.byref(d), *p[:4], FREQ, place, *p[4:10], None, 0, None)
 
@@ -29,6 +31,7 @@ def test_rows_beyond_64_bits(big):
     # an axis of one element may have any stride, and so may keys that there are not
     one = ((1 << 63) - 1, 256, 64)
     assert _call("bwd", B=1, q_strides=one, k_strides=one, dq_strides=one, dk_strides=one) == ra.RACE_ERR_WORKSPACE
+    assert _call("bwd", Hk=0, k_strides=big, dk_strides=big) == ra.RACE_ERR_WORKSPACE
 
 
 def test_positions_beyond_64_bits():
