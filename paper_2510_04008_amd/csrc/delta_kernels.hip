@@ -615,9 +615,9 @@ __global__ __launch_bounds__(THREADS) void delta_scan_kernel(ScanArgs a)
 // ------------------------------------------------------------------ states at the segments' starts
 // S <- P_s S + B_s, segment after segment (REV: from the last to the first, with P_s^T).  One workgroup per head and 16 COLS columns, a
 // wavefront per 16 rows; the new rows reach the other wavefronts as operands through LDS, one barrier a step (two buffers), and P and B are
-// asked for two steps ahead (three: no faster).  A step takes 2 us all the same, a chain of LDS, barrier and products one after the other, so many segments
-// are joined in groups of about the root of their number: the transitions of the groups side by side (compose), the groups one after the other, then the segments of all groups side by side.
-// 63 transitions of four heads, dk = dv = 128, bf16: 66 us in the three launches, 130 would be one after the other.
+// asked for two steps ahead (three: no faster).  A step takes 1.6 us all the same (dk = 64: 0.8), a chain of LDS, barrier and products one after the other, so many segments
+// of few heads (joined_in_groups) are joined in groups of about the root of their number: the transitions of the groups side by side (compose), the groups one after the other,
+// then the segments of all groups side by side.  64 transitions of four heads, dk = dv = 128, bf16: 59 us in the three launches, 106 one after the other.
 struct CombineArgs {
     Sizes z;
     int heads, groups, each;        // transitions of a group: each; the last group's may be fewer
@@ -1543,7 +1543,7 @@ struct Passes {
         a.carry_head = carry_head;
         a.at = rev ? floats(ws, p.off_end) : floats(ws, p.off_start) + z.seg0 * one;
         a.at_head = one * (rev ? p.win_segs : p.nseg + 1);
-        if (p.join_groups > 1 && steps >= kJoinInGroups) {
+        if (joined_in_groups(steps, p.BH)) {
             const int each = (steps + p.join_groups - 1) / p.join_groups, groups = (steps + each - 1) / each;
             // the groups' transitions; the last group's is nobody's
             CombineArgs c = a;

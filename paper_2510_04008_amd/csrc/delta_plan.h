@@ -8,8 +8,11 @@
 namespace race {
 namespace delta {
 
-// Fewer transitions than these are joined one after the other: three launches of the root of their number of steps each take no less.
-constexpr int kJoinInGroups = 12;
+// Whether `steps` transitions of BH heads are joined in groups (delta_combine_kernel) and not one after the other.  In groups there are three short chains for a long
+// one, but every group's transitions are multiplied with one another, which fills the chip from some eight heads on.  Measured, us, one after the other / in groups,
+// 128 x 128, bf16:  4 heads: 16 steps 31 / 37, 20: 37 / 38, 24: 44 / 41, 64: 106 / 59;  8 heads: 24: 43 / 49, 32: 56 / 59, 48: 81 / 67;  16 heads: 64: 108 / 129,
+// 128: 324 / 308;  32 heads: 128: 359 / 566.  64 x 64: 4 heads: 24: 23 / 26, 32: 30 / 29;  16 heads: 32: 29 / 32, 48: 41 / 36.
+inline bool joined_in_groups(int steps, int BH) { return BH <= 16 && steps >= 24 && 2 * steps >= BH * BH; }
 
 struct DeltaPlan {
     int B, H, Hk, BH, dk, dv, dvp, dtype;       // dvp: dv rounded up to 32

@@ -11,7 +11,7 @@
 namespace race {
 namespace {
 
-using delta::kJoinInGroups;
+using delta::joined_in_groups;
 
 constexpr int kChunk = 64;
 constexpr int kMaxHeads = 65535;            // B H: a grid dimension
@@ -40,17 +40,19 @@ race_status_t check_delta(const race_delta_desc_t *d)
     return RACE_OK;
 }
 
-// Segments that run side by side, by the time of a forward pass, in us, from sweeps at dk = dv = 128 (bf16; the other shapes have their minimum
-// in the same places): a chunk takes 7.2 in the pass proper, with a workgroup per segment and head, and 4.4 in the pre-pass, with two; the CUs hold
-// 256 workgroups at once; the join takes 2 to 3 a segment one after the other, in groups 25 + 0.7 a segment.  At B H = 4 and 1024 chunks, training: 64 segments
-// 1521, 61: 1556, 52: 1660, 43: 1807, 32: 1895, 74 (a second round): 1931.
+// Segments that run side by side, by the time of a forward pass, in us, at dk = dv = 128, bf16: a chunk takes 7.9 in the pass proper, with a workgroup per segment and
+// head, and 4.3 in the pre-pass, with two; the CUs hold 256 workgroups at once; the join takes 5 + 1.6 a segment one after the other, 30 + 0.45 in groups.
+// Sweeps of training steps and prompts over 1 to 128 segments, us, the rule's choice first:  training, 4 heads x 65536 tokens: 64 segments 1584, 47: 1792, 74 (a
+// second round): 1996;  16 x 10007, 64 x 128: 16: 799, 14: 810, 32: 823;  4 x 8192, fp32: 64: 671, 32: 766, 128: 875;  8 x 2003, 64 x 64, fp32: 16: 220, 8: 294, 32: 227.
+// Prompts, 4 x 30011: 59: 249, 47: 247;  8 x 16384, 128 x 64: 32: 215, 24: 234, 43: 251;  32 x 8192: 8: 350, 6: 403, 13: 359;  64 x 4096: 4: 320, 3: 321;  128 x 2048:
+// 2: 296, 1: 276.
 int choose_segments(int chunks, int BH)
 {
     int best = 1;
-    double cost = 7.2 * chunks;
+    double cost = 7.9 * chunks;
     for (int n = 2; n <= 256 / BH && n <= chunks; ++n) {
         const int m = (chunks + n - 1) / n, rounds = (2 * (n - 1) * BH + 255) / 256;
-        const double c = (7.2 + 4.4 * rounds) * m + (n <= kJoinInGroups ? 3.0 * n : 25.0 + 0.7 * n) + 12.0;
+        const double c = (7.9 + 4.3 * rounds) * m + (joined_in_groups(n - 1, BH) ? 30.0 + 0.45 * n : 5.0 + 1.6 * n) + 12.0;
         if (c < cost) {
             cost = c;
             best = n;
@@ -106,7 +108,7 @@ race_status_t plan_delta(const race_delta_desc_t *d, bool backward, delta::Delta
         p.off_add = take(segs * one);
         p.off_P = take(segs * dkp * dkp * 4);
     }
-    if (p.win_segs > kJoinInGroups) {
+    if (joined_in_groups(p.win_segs, p.BH)) {
         p.join_groups = static_cast<int>(std::lround(std::sqrt(static_cast<double>(p.win_segs))));
         p.off_group_P = take(static_cast<size_t>(p.BH) * p.join_groups * dkp * dkp * 4);
         p.off_group_add = take(static_cast<size_t>(p.BH) * p.join_groups * one);
