@@ -1707,12 +1707,15 @@ struct Passes {
     }
 };
 
-// Eight wavefronts where there are columns or rows for them: a workgroup of four has half the tiles to stage and fits a CU twice.
+// Eight wavefronts, also where four would hold all columns of the state and the others only stage rows and images; fp32 takes four then.  Training, 64 x 64, us with eight /
+// with four:  bf16, 4 heads x 65536 tokens: 910 / 939 (a prompt: 199 / 214), 32 x 8192: 804 / 848;  fp32, 32 x 8192: 1400 / 1393, 8 x 2003: 240 / 230.
 template <class X, class F>
 hipError_t for_width(const DeltaPlan &p, F f)
 {
     if (p.dk > 64) return f(Passes<X, 128, 512>());
-    return p.dvp > 64 ? f(Passes<X, 64, 512>()) : f(Passes<X, 64, 256>());
+    if constexpr (sizeof(typename X::E) == 4)
+        if (p.dvp <= 64) return f(Passes<X, 64, 256>());
+    return f(Passes<X, 64, 512>());
 }
 template <class F>
 hipError_t for_shape(const DeltaPlan &p, F f) { return p.dtype == RACE_BF16 ? for_width<Bf>(p, f) : for_width<Fp>(p, f); }
