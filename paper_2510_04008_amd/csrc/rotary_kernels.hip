@@ -23,8 +23,9 @@ namespace rotary {
 namespace {
 
 constexpr int kThreads = 256;
-// Workgroups of the forward pass in a grid's first dimension, which has to stay below 2^32 threads: beyond them a group takes several tokens.
-constexpr int64_t kMaxBlocks = 1 << 20;
+// Workgroups of a launch of the forward pass: a grid's dimension has to stay below 2^32 threads, so more tokens take several launches.  (A loop over tokens
+// in the kernel instead cost a tenth of its time: 262144 tokens of 8 + 8 heads, d = 128, 491 us against 446.)
+constexpr int64_t kMaxBlocks = 1 << 23;
 
 template <class E, int W> struct Run;       // W elements as they lie in memory; a caller's rows are aligned to their elements only
 template <> struct Run<uint16_t, 4> { typedef __attribute__((ext_vector_type(4), aligned(2))) uint16_t T; };
@@ -145,37 +146,36 @@ __device__ __forceinline__ float scale_of(const RotaryPlan &p, float squares)
 }
 
 template <class E, int W, int NU>
-__global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(RotaryPlan p, int lanes, int heads_each)
+__global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(RotaryPlan p, int lanes, int heads_each, int64_t token0)
 {
     const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
     const int64_t tokens = static_cast<int64_t>(p.B) * p.N;
+    const int64_t token = token0 + static_cast<int64_t>(blockIdx.x) * groups + threadIdx.x / lanes;
+    if (token >= tokens) return;            // whole groups: the sums over a group's lanes stay complete
+    const int64_t b = token / p.N, n = token - b * p.N;
     Lane<W, NU> l;
     l.place(p, lane, lanes);
+    l.turn(p, lane, lanes, p.positions ? p.positions[token] : p.pos0 + n);
     const int first = blockIdx.y * heads_each, last = min(first + heads_each, p.q.heads + p.k.heads);
-    // (a group's lanes have the same token: the sums over them stay complete)
-    for (int64_t token = static_cast<int64_t>(blockIdx.x) * groups + threadIdx.x / lanes; token < tokens; token += static_cast<int64_t>(gridDim.x) * groups) {
-        const int64_t b = token / p.N, n = token - b * p.N;
-        l.turn(p, lane, lanes, p.positions ? p.positions[token] : p.pos0 + n);
-        for (int hh = first; hh < last; ++hh) {
-            const bool isq = hh < p.q.heads;
-            const Rows &r = isq ? p.q : p.k;
-            const int h = isq ? hh : hh - p.q.heads;
-            float x[NU][2 * W], w[NU][2 * W];
-            l.row(static_cast<const E *>(r.x) + b * r.batch + n * r.token + h * r.head, x);
-            float ss = 0.f;
+    for (int hh = first; hh < last; ++hh) {
+        const bool isq = hh < p.q.heads;
+        const Rows &r = isq ? p.q : p.k;
+        const int h = isq ? hh : hh - p.q.heads;
+        float x[NU][2 * W], w[NU][2 * W];
+        l.row(static_cast<const E *>(r.x) + b * r.batch + n * r.token + h * r.head, x);
+        float ss = 0.f;
 #pragma unroll
-            for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int e = 0; e < 2 * W; ++e) ss += x[u][e] * x[u][e];
-            const float scale = scale_of(p, p.norm ? over_group(ss, lanes) : 0.f);
-            if (r.w) l.row(r.w, w);
+            for (int e = 0; e < 2 * W; ++e) ss += x[u][e] * x[u][e];
+        const float scale = scale_of(p, p.norm ? over_group(ss, lanes) : 0.f);
+        if (r.w) l.row(r.w, w);
 #pragma unroll
-            for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int e = 0; e < 2 * W; ++e) x[u][e] *= r.w ? scale * w[u][e] : scale;
-            l.rotate(p, x, 1.f);
-            l.put_row(static_cast<E *>(r.y) + ((b * r.heads + h) * p.N + n) * p.d, x);
-        }
+            for (int e = 0; e < 2 * W; ++e) x[u][e] *= r.w ? scale * w[u][e] : scale;
+        l.rotate(p, x, 1.f);
+        l.put_row(static_cast<E *>(r.y) + ((b * r.heads + h) * p.N + n) * p.d, x);
     }
 }
 
@@ -284,13 +284,16 @@ template <class E, int W, int NU>
 hipError_t launch_fwd(const RotaryPlan &p, hipStream_t st)
 {
     const int lanes = lanes_of(p, W), groups = kThreads / lanes, heads = p.q.heads + p.k.heads;
-    const int64_t blocks = std::min<int64_t>(kMaxBlocks, (static_cast<int64_t>(p.B) * p.N + groups - 1) / groups);
+    const int64_t blocks = (static_cast<int64_t>(p.B) * p.N + groups - 1) / groups;
     int each = heads;       // fewer heads a group where there are few tokens
     while (each > 1 && blocks * ((heads + each - 1) / each) < 1024) each = (each + 1) / 2;
-    const dim3 grid(static_cast<unsigned>(blocks), (heads + each - 1) / each);
-    ProfileScope scope("rotary_fwd", st);
-    rotary_fwd_kernel<E, W, NU><<<grid, kThreads, 0, st>>>(p, lanes, each);
-    return hipGetLastError();
+    for (int64_t first = 0; first < blocks; first += kMaxBlocks) {
+        const dim3 grid(static_cast<unsigned>(std::min(kMaxBlocks, blocks - first)), (heads + each - 1) / each);
+        ProfileScope scope("rotary_fwd", st);
+        rotary_fwd_kernel<E, W, NU><<<grid, kThreads, 0, st>>>(p, lanes, each, first * groups);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 template <class E, int W, int NU>
 hipError_t launch_bwd(const RotaryPlan &p, float *parts, hipStream_t st)
