@@ -230,8 +230,7 @@ race_status_t race_attn_step(const race_attn_desc_t *desc, const void *q, const 
  *     outputs and, where its dO is 0, gradients.  Its own output reads the state with its query, whose products with keys and states have to stay finite.
  *     Its rows of dK and dV are 0; its dbeta is what the formula makes of its rows.
  *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64; a sum over part of 64 tokens has to stay
- *     below 88, where exp leaves fp32).  The bf16 type multiplies fp32 values as sums of three bf16, all 24 bits (of two where only a bf16 output depends
- *     on the product); O, dQ, dK and dV are rounded to bf16 at the end.
+ *     below 88, where exp leaves fp32).  The bf16 type multiplies fp32 values as sums of three bf16, all 24 bits; O, dQ, dK and dV are rounded to bf16 at the end.
  *   - A non-finite element of Q, K, V or dO reaches what depends on it, and may spread over the 64 tokens of its chunk, for bf16 and
  *     fp32 alike; it does not reach another head or sequence (Q, K: other than those that share them).
  *   - Pointers need be aligned to their elements only.  Buffers must not overlap, except that a state may be carried in place: state_out

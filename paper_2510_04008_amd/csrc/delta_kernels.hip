@@ -49,8 +49,8 @@ __device__ __forceinline__ void kept8(const float *p, float *x)
 // alike the powers reach thousands where T stays near one.
 // Images are written in the order in which the scans' operands lie in LDS (rows in spread order), in fp32: half of the bytes of a Split.
 // One workgroup of four wavefronts per chunk and head, several on a CU, so that one's substitution (16 steps of one wavefront) runs beside another's loads.  65536 chunks
-// of dk = 128, bf16 (2^20 tokens, four heads): 686 us, 34 KB a chunk and 3.3 TB/s; wavefronts wait 70 % of their time, for loads and
-// at the barriers between the steps.
+// of dk = 128, bf16 (2^20 tokens, four heads): 658 us, 34 KB a chunk and 3.4 TB/s; wavefronts wait 75 % of their time, for loads and
+// at the barriers between the steps.  With what the way back needs, 80 KB a chunk, 4096 chunks take 88 us.
 template <int SIZE>
 struct MergeBlocks {
     static constexpr int NT = SIZE / 16;
@@ -398,11 +398,12 @@ __device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state,
 // accumulators from chunk to chunk (DK x 16 fp32), where they are at once the right operand of the products with K and Q.
 // Columns never meet, so wavefronts share the tiles in LDS and nothing else.
 //
-// What bounds it is the issue of instructions: at dk = dv = 128, bf16, the matrix units are busy 40 to 47 % of the time and the vector ALU, which splits states,
-// R and U into bf16 for the next product, 48 to 58 % (the issue of matrix instructions included); the state's columns in registers (up to 252 a lane) leave room for two wavefronts a SIMD.  Sixteen columns a
-// wavefront and eight wavefronts beat 32 columns and four (one wavefront a SIMD: nothing to fill its waits).  Tried without gain: operands asked for before
+// A chunk is a chain of products, each of which needs the one before it, and no unit is saturated: at dk = dv = 128, bf16, the matrix units are busy 41 to 47 % of the time, the
+// vector ALU, which splits states, R and U into bf16 for the next product, 49 to 61 % (the issue of matrix instructions included), LDS 32 to 48 % (bank conflicts 14 to 21),
+// and wavefronts wait 22 to 32 %; the state's columns in registers (up to 248 a lane) leave room for two wavefronts a SIMD to fill the gaps.  (fp32, 64 x 64: matrix units 43
+// to 49 %, vector ALU 17, waiting 28 to 38.)  Sixteen columns a wavefront and eight wavefronts beat 32 columns and four (one wavefront a SIMD: nothing to fill its waits).  Tried without gain: operands asked for before
 // the split of the state, and priorities for the matrix phases or for half of the wavefronts.  2^20 tokens, four heads, 64 segments, so a workgroup
-// on every CU: 1.90 ms, 7.4 us a chunk; the pre-pass, two workgroups a segment: 2.28 ms; kKeep, 96 KB a chunk more to write, takes 7.4 us a chunk too.
+// on every CU: 2.02 ms, 7.9 us a chunk; the pre-pass, two workgroups a segment: 2.21 ms; kKeep, 96 KB a chunk more to write, takes 7.2 us a chunk.
 enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's transition and state from zero; states and U for the backward pass
 
 struct ScanArgs {
@@ -734,8 +735,8 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(CombineArgs a)
 }
 
 // ------------------------------------------------------------------ cotangents of the states, last chunk first
-// The scan's mirror image: the same split of the work, the same bound (matrix units busy 31 to 36 %, vector ALU 35 to 42 %, two wavefronts a SIMD, and more to
-// stage and to write), 11.7 us a chunk with dV and what the gradients read (FULL: 96 KB a chunk), 8.5 us without, at dk = dv = 128, bf16.
+// The scan's mirror image: the same split of the work, as little saturated (matrix units busy 31 to 36 %, vector ALU 37 to 45 %, waiting 31 to 33 %, two wavefronts a SIMD, and more to
+// stage and to write), 11.8 us a chunk with dV and what the gradients read (FULL: 96 KB a chunk), 8.5 us without, at dk = dv = 128, bf16.
 struct RevArgs {
     Sizes z;
     const void *Q, *K, *dO;
@@ -964,8 +965,9 @@ __device__ __forceinline__ float prefix16(float x)
 // chunk before it, whose states it has asked for by then.
 // dg: W = M o (dO U^T) - A o (dR U^T) lies in the same 16 x 16 tiles as F and E, rows j in registers and columns i in lanes.  A tile's sums over i >= t are four
 // steps over the lanes; below the diagonal they and the sums of its rows j are all that dg needs of it (kPairs), and one wavefront adds up a chunk's.
-// 4096 chunks of dk = dv = 128, bf16: 342 us for 288 KB a chunk, 3.5 TB/s.  LDS holds one workgroup of a CU, which waits for its own reading at the chunk's start
-// and for tiles in LDS after that.
+// 4096 chunks of dk = dv = 128, bf16: 425 us for 1.32 GB, 3.1 TB/s; matrix units busy 19 % of the time, vector ALU 34 %, LDS 35 %, waiting 31 %.  LDS holds one workgroup of
+// a CU, which waits for its own reading at the chunk's start and for tiles in LDS after that.  (dR and dS as three
+// bf16 and not two cost 12 % of the kernel, the sums for dg another 12.)
 constexpr int kGradThreads = 512;
 
 template <class X, int DK>
