@@ -232,7 +232,8 @@ race_status_t race_attn_step(const race_attn_desc_t *desc, const void *q, const 
  *   - Chunks of 64 tokens are worked on at once; state, sums and decays are held in fp32 (decays are summed in fp64; a sum over part of 64 tokens has to stay
  *     below 88, where exp leaves fp32).  The bf16 type multiplies fp32 values as sums of three bf16, all 24 bits; O, dQ, dK and dV are rounded to bf16 at the end.
  *   - A non-finite element of Q, K, V or dO reaches what depends on it, and may spread over the 64 tokens of its chunk, for bf16 and
- *     fp32 alike; it does not reach another head or sequence (Q, K: other than those that share them).
+ *     fp32 alike; it does not reach another head or sequence (Q, K: other than those that share them).  (The dbeta of a token of strength zero may stay finite: what its
+ *     key makes of cotangents is cut off at 2^60.)
  *   - Pointers need be aligned to their elements only.  Buffers must not overlap, except that a state may be carried in place: state_out
  *     may be state_in, dstate_in may be dstate_out.
  *   - Everything else (workspace, streams, errors, capture into a graph) as above.  Results are the same bits every time. */
@@ -253,7 +254,8 @@ size_t race_delta_workspace_bytes(const race_delta_desc_t *desc);
 size_t race_delta_bwd_workspace_bytes(const race_delta_desc_t *desc);
 /* Bytes of one state (B, H, dk, dv are used); 0 for an invalid descriptor. */
 size_t race_delta_state_bytes(const race_delta_desc_t *desc);
-/* Tokens per scan segment the library uses for this descriptor.  Informational.  0 = invalid. */
+/* Tokens per scan segment that race_delta_fwd uses for this descriptor (race_delta_bwd chooses its own with chunk = 0: its windows hold fewer chunks).
+ * Informational.  0 = invalid. */
 int64_t race_delta_segment_tokens(const race_delta_desc_t *desc);
 
 /* Forward pass.  state_in: state before the first token, NULL = zero.  state_out: state behind the last token, NULL = not wanted.
