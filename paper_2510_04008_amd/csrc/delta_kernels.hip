@@ -401,8 +401,8 @@ __device__ __forceinline__ void put_state(const f32x4 (&S)[TILES], float *state,
 // A chunk is a chain of products, each of which needs the one before it, and no unit is saturated: at dk = dv = 128, bf16, the matrix units are busy 41 to 47 % of the time, the
 // vector ALU, which splits states, R and U into bf16 for the next product, 49 to 61 % (the issue of matrix instructions included), LDS 32 to 48 % (bank conflicts 14 to 21),
 // and wavefronts wait 22 to 32 %; the state's columns in registers (up to 248 a lane) leave room for two wavefronts a SIMD to fill the gaps.  (fp32, 64 x 64: matrix units 43
-// to 49 %, vector ALU 17, waiting 28 to 38.)  Sixteen columns a wavefront and eight wavefronts beat 32 columns and four (one wavefront a SIMD: nothing to fill its waits).  Tried without gain: operands asked for before
-// the split of the state, and priorities for the matrix phases or for half of the wavefronts.  2^20 tokens, four heads, 64 segments, so a workgroup
+// to 49 %, vector ALU 17, waiting 28 to 38.)  Sixteen columns a wavefront and eight wavefronts beat 32 columns and four (one wavefront a SIMD: nothing
+// to fill its waits).  Tried without gain: operands asked for before the split of the state, and priorities for the matrix phases or for half of the wavefronts.  2^20 tokens, four heads, 64 segments, so a workgroup
 // on every CU: 2.02 ms, 7.9 us a chunk; the pre-pass, two workgroups a segment: 2.21 ms; kKeep, 96 KB a chunk more to write, takes 7.2 us a chunk.
 enum ScanMode { kOut, kPre, kKeep };        // the pass proper; a segment's transition and state from zero; states and U for the backward pass
 
